@@ -55,7 +55,8 @@
 extern "C" {
 #endif
 
-typedef enum { QLORA_F16 = 0, QLORA_BF16 = 1 } qlora_dtype_t;
+/* QLORA_F32 is accepted by the calls that say so (token log probabilities, optimizer), by no other. */
+typedef enum { QLORA_F16 = 0, QLORA_BF16 = 1, QLORA_F32 = 2 } qlora_dtype_t;
 
 typedef enum {
     QLORA_OK = 0,
@@ -64,12 +65,14 @@ typedef enum {
     QLORA_E_SHAPE = 3,      /* M < 1, K % 32 != 0, N % 8 != 0, or a size overflows */
     QLORA_E_GROUP = 4,      /* group_size % 32 != 0 or K % group_size != 0 */
     QLORA_E_RANK = 5,       /* rank not in {0, 8, ..., 64} */
-    QLORA_E_DTYPE = 6,      /* dtype not QLORA_F16 / QLORA_BF16 */
+    QLORA_E_DTYPE = 6,      /* dtype not QLORA_F16 / QLORA_BF16 (or QLORA_F32, for the calls that take it) */
     QLORA_E_ALIGN = 7,      /* a pointer is not 16-byte aligned */
     QLORA_E_WORKSPACE = 8,  /* workspace NULL or smaller than qlora_workspace_bytes() */
     QLORA_E_HIP = 9,        /* the HIP runtime reported an error at launch */
     QLORA_E_GIDX = 10,      /* a group index is out of range, or a group does not own exactly group_size columns */
-    QLORA_E_STATIC = 11     /* qlora_linear_fwd_static: the problem needs more scratch than QLORA_STATIC_SCRATCH_BYTES */
+    QLORA_E_STATIC = 11,    /* qlora_linear_fwd_static: the problem needs more scratch than QLORA_STATIC_SCRATCH_BYTES */
+    QLORA_E_PLAN = 12,      /* not a plan of qlora_optim_plan, a plan without weights, or tensors that overlap */
+    QLORA_E_VALUE = 13      /* a number (beta, eps, norm, stride, count of alternatives) is out of its range */
 } qlora_status_t;
 
 /* Host pointer to a static, NUL-terminated description of `status`. */
@@ -362,6 +365,126 @@ int qlora_lrec_loss_scaled(const void *student_logits, const void *teacher_logit
                            float lambda_kl, float lambda_ce, float grad_scale, float *kl, float *ce,
                            float *loss_mean, void *dlogits, int M, int V, int dtype,
                            void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Log probabilities of given tokens, with entropy and the most likely alternatives: what a quantized model is
+ * evaluated on (perplexity, Sec. 4), what serving reports beside the tokens it generates, and what sequence-level
+ * objectives are made of.  Per row m of logits z [M,V] (of `dtype`: fp16, bf16 or QLORA_F32), rows `row_stride` >= V
+ * elements apart:
+ *     log p_i = z_i - ln sum_j exp(z_j)
+ *     logprob[m] = log p of tokens[m]; 0 where tokens[m] is negative or not below V (nothing given there)
+ *     entropy[m] = -sum_i p_i log p_i
+ *     alt_tokens[m, 0..k), alt_logprobs[m, 0..k): the k = `alternatives` largest log p in descending order, the
+ *         lower token first where two are equal; k <= QLORA_MAX_ALTERNATIVES, 0: none (both pointers are ignored)
+ *     stats [M,4]: largest logit, S = sum of exp(z - largest), ln S, entropy: what qlora_token_logprobs_bwd needs
+ * Each output is fp32 (tokens int32) and may be NULL; tokens is needed for logprob only.  At least one output is asked for.
+ *
+ * Minus infinity masks a token: its probability is 0, log p is -inf, and it is no alternative (places left over hold
+ * token -1 and -inf).  A row that masks every token has log p = -inf everywhere, entropy 0 and no alternatives.  A NaN
+ * or plus infinity in a row makes its logprob, entropy, alt_logprobs and stats NaN and its alt_tokens -1.
+ *
+ * logits and stats are 16-byte aligned, the other pointers 4; V >= 1, M < 2^22, M*V < 2^35, M*row_stride < 2^40.
+ * workspace: qlora_token_logprobs_workspace_bytes(M, V, alternatives, dtype) bytes; NULL is accepted where that is 0
+ * because rows are short (a call with bad arguments says so itself).  Sums run in a fixed order: results are bitwise
+ * reproducible.
+ */
+#define QLORA_MAX_ALTERNATIVES 64
+size_t qlora_token_logprobs_workspace_bytes(int M, int V, int alternatives, int dtype);
+
+int qlora_token_logprobs(const void *logits, int64_t row_stride, const int32_t *tokens, float *logprob, float *entropy,
+                         int32_t *alt_tokens, float *alt_logprobs, int alternatives, float *stats,
+                         int M, int V, int dtype, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Its gradient:  dlogits[m,i] = g ([i = tokens[m]] - p_i) - h p_i (log p_i + entropy),  g = d_logprob[m] (0 where no
+ * token is given), h = d_entropy[m]; written in `dtype`, entries beyond V of a wider row are left alone.  logits,
+ * row_stride and tokens as in the forward call, stats as it wrote them.  d_logprob [M] with tokens, or d_entropy [M], may
+ * be NULL (no such gradient), not both.  A masked token has p = 0.  Where g and h are both 0 the row is zeros whatever its
+ * logits are.  dlogits may be logits itself with the same stride (the gradient then replaces them), and
+ * overlaps them in no other way.
+ */
+int qlora_token_logprobs_bwd(const void *logits, int64_t row_stride, const int32_t *tokens, const float *stats,
+                             const float *d_logprob, const float *d_entropy, void *dlogits, int64_t d_row_stride,
+                             int M, int V, int dtype, void *stream);
+
+/*
+ * The adapters' optimizer (Appendix B trains with AdamW): one step over all tensors of a training program, with the
+ * gradients as the backward calls leave them (dA, dB in fp32; QLORA_F16 / QLORA_BF16 ones are taken too).
+ *     g = grad * grad_scale * clip
+ *     exp_avg    m = beta1 m + (1 - beta1) g          exp_avg_sq  v = beta2 v + (1 - beta2) g^2
+ *     w = w (1 - lr' weight_decay) - lr' / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps),  lr' = lr * lr_scale
+ * lr, grad_scale (1 / the loss scale of qlora_lrec_loss_scaled), the seed and the number t of steps taken live in a
+ * control block in device memory: a captured step can be replayed while the program writes a new lr into it.
+ *
+ * A tensor: `param` [numel] of param_dtype (fp16, bf16 or QLORA_F32).  With `master` (fp32 [numel], 16-bit param only)
+ * the step moves master and param receives its rounding; without it w is read from param and rounded to nearest, which
+ * loses steps below half the distance of two numbers of that type.  States of 32 bits: exp_avg and exp_avg_sq are fp32
+ * [numel], the scales are not read.  States of 8 bits: both hold one e4m3 code a weight, exp_avg of m and exp_avg_sq of
+ * sqrt(v), and avg_scale / avg_sq_scale [ceil(numel / QLORA_OPTIM_BLOCK)] fp32 the power of two that each
+ * run of QLORA_OPTIM_BLOCK codes is multiplied by.  Codes are rounded up or down at random, with odds that keep the mean:
+ * the random bits are a hash of seed, step and the weight's place in the plan, so runs repeat bit by bit; a second
+ * moment above 0 keeps a code above 0.  All states start as zero bytes.
+ * param, grad, master and the states are 16-byte aligned, the scales 4.  What the step writes overlaps nothing else in
+ * the plan (QLORA_E_PLAN).  numel 0 is a tensor without weights; its pointers are ignored.  param NULL: the tensor has a
+ * gradient only, and the plan serves qlora_grad_norm alone.
+ */
+#define QLORA_OPTIM_BLOCK 256
+typedef struct {
+    void *param;
+    const void *grad;
+    float *master;
+    void *exp_avg, *exp_avg_sq;
+    float *avg_scale, *avg_sq_scale;
+    int64_t numel;                  /* 0 <= numel <= 2^36 */
+    float lr_scale, weight_decay;   /* finite, not negative */
+    int32_t param_dtype, grad_dtype;
+    int32_t state_bits;             /* 8 or 32 */
+    int32_t reserved;               /* 0 */
+} qlora_optim_tensor_t;
+
+/*
+ * The plan of a set of tensors, HOST memory: made once (the pointers are part of it, so again when a buffer moves),
+ * then copied as it is to 16-byte aligned device memory by the caller, who keeps both.  qlora_optim_plan_bytes: its
+ * size, 0 if numbers of weights are out of range or all are 0.  QLORA_E_WORKSPACE if plan_bytes is smaller.
+ */
+size_t qlora_optim_plan_bytes(int count, const qlora_optim_tensor_t *tensors);
+int qlora_optim_plan(int count, const qlora_optim_tensor_t *tensors, void *plan, size_t plan_bytes);
+
+/* The control block, DEVICE memory of the caller, 16-byte aligned; filled on the host by qlora_optim_control_init. */
+typedef struct {
+    float lr, grad_scale;           /* the caller's: read by every step */
+    uint32_t seed;                  /* the caller's: 8-bit states */
+    int32_t step;                   /* steps taken */
+    int32_t skipped;                /* calls that took none because the gradients were not finite */
+    float grad_norm;                /* of the last call that looked, times grad_scale, before clipping */
+    float rate, root;               /* of the step under way: lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t) */
+    double beta1_power, beta2_power;        /* beta^step */
+    uint32_t key, reserved[3];
+} qlora_optim_control_t;
+/* HOST memory: a control block after `step` steps (0: a fresh start).  QLORA_E_VALUE: a beta outside [0, 1), step < 0. */
+int qlora_optim_control_init(qlora_optim_control_t *control, float lr, float grad_scale, uint32_t seed, int32_t step,
+                             double beta1, double beta2);
+
+/* Bytes of device scratch that qlora_grad_norm and qlora_adamw_step need, 16-byte aligned. */
+size_t qlora_optim_workspace_bytes(void);
+
+/*
+ * norm[0] = |grad_scale| * sqrt(sum of the squares of all gradients of the plan), fp32, DEVICE; summed in 64 bits
+ * in a fixed order.  Inf or NaN if a gradient is.
+ */
+int qlora_grad_norm(const void *plan, const void *plan_device, float grad_scale, float *norm, void *workspace,
+                    size_t workspace_bytes, void *stream);
+
+/*
+ * One step.  max_grad_norm > 0: the norm is taken first, control->grad_norm receives it, the gradients are scaled
+ * by clip = min(1, max_grad_norm / norm), and if the norm is not finite (an overflow under loss scaling) nothing changes but
+ * control->skipped and grad_norm; INFINITY checks without clipping.  max_grad_norm == 0: neither; the workspace
+ * may then be NULL, clip is 1, and a gradient that is not finite makes its weight and states NaN (8-bit states: its
+ * block's).  Gradients are not cleared.  QLORA_E_VALUE: a beta outside [0, 1), eps or max_grad_norm negative or NaN.
+ * Calls that share a control block or a workspace and overlap in time race.  Two launches.
+ */
+int qlora_adamw_step(const void *plan, const void *plan_device, qlora_optim_control_t *control, double beta1, double beta2,
+                     double eps, double max_grad_norm, void *workspace, size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

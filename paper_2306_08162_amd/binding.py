@@ -14,9 +14,10 @@ from typing import Optional
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libqlora.so")
 
-QLORA_F16, QLORA_BF16 = 0, 1
+QLORA_F16, QLORA_BF16, QLORA_F32 = 0, 1, 2
 STATUS_NAMES = ["QLORA_OK", "QLORA_E_NULL", "QLORA_E_BITS", "QLORA_E_SHAPE", "QLORA_E_GROUP", "QLORA_E_RANK",
-                "QLORA_E_DTYPE", "QLORA_E_ALIGN", "QLORA_E_WORKSPACE", "QLORA_E_HIP", "QLORA_E_GIDX", "QLORA_E_STATIC"]
+                "QLORA_E_DTYPE", "QLORA_E_ALIGN", "QLORA_E_WORKSPACE", "QLORA_E_HIP", "QLORA_E_GIDX", "QLORA_E_STATIC",
+                "QLORA_E_PLAN", "QLORA_E_VALUE"]
 STATIC_SCRATCH_BYTES = 32 << 20
 EXPORTS = ["qlora_status_string", "qlora_packed_words", "qlora_workspace_bytes", "qlora_pack", "qlora_unpack",
            "qlora_actorder_perm", "qlora_pack_permuted", "qlora_gather_columns",
@@ -24,14 +25,36 @@ EXPORTS = ["qlora_status_string", "qlora_packed_words", "qlora_workspace_bytes",
            "qlora_linear_fwd", "qlora_linear_bwd", "qlora_linear_bwd_accumulate", "qlora_linear_fwd_dropout",
            "qlora_linear_bwd_dropout", "qlora_linear_bwd_stacked", "qlora_linear_bwd_dropout_stacked", "qlora_siblings_workspace_bytes", "qlora_linear_fwd_siblings",
            "qlora_linear_bwd_siblings", "qlora_lrec_workspace_bytes", "qlora_lrec_loss", "qlora_lrec_loss_scaled", "qlora_linear_fwd_static",
-           "qlora_workspace_bytes_zp", "qlora_linear_fwd_zp", "qlora_linear_bwd_zp"]
+           "qlora_workspace_bytes_zp", "qlora_linear_fwd_zp", "qlora_linear_bwd_zp",
+           "qlora_token_logprobs_workspace_bytes", "qlora_token_logprobs", "qlora_token_logprobs_bwd",
+           "qlora_optim_plan_bytes", "qlora_optim_plan", "qlora_optim_control_init", "qlora_optim_workspace_bytes",
+           "qlora_grad_norm", "qlora_adamw_step"]
 BENCH_EXPORTS = ["qlora_profile_gemm", "qlora_profile_gemm_span", "qlora_stream_probe", "qlora_mfma_probe"]        # include/qlora_bench.h
 STREAM_PROBE_WORDS = 1024
 MFMA_PROBE_FLOATS = 256 * 512              # floats of the probe's output
 MFMA_PROBE_FLOP_PER_ITER = 256 * 8 * 16 * 16384  # per round: workgroups x waves x MFMAs x flop of a 16x16x32 MFMA
 MAX_SIBLINGS, SIBLINGS_MAX_M = 4, 16
+MAX_ALTERNATIVES = 64
+OPTIM_BLOCK = 256
 
 _lib = None
+
+
+class OptimTensorStruct(ctypes.Structure):
+    """qlora_optim_tensor_t"""
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("master", ctypes.c_void_p),
+                ("exp_avg", ctypes.c_void_p), ("exp_avg_sq", ctypes.c_void_p), ("avg_scale", ctypes.c_void_p),
+                ("avg_sq_scale", ctypes.c_void_p), ("numel", ctypes.c_int64), ("lr_scale", ctypes.c_float),
+                ("weight_decay", ctypes.c_float), ("param_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32),
+                ("state_bits", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class OptimControlStruct(ctypes.Structure):
+    """qlora_optim_control_t"""
+    _fields_ = [("lr", ctypes.c_float), ("grad_scale", ctypes.c_float), ("seed", ctypes.c_uint32),
+                ("step", ctypes.c_int32), ("skipped", ctypes.c_int32), ("grad_norm", ctypes.c_float),
+                ("rate", ctypes.c_float), ("root", ctypes.c_float), ("beta1_power", ctypes.c_double),
+                ("beta2_power", ctypes.c_double), ("key", ctypes.c_uint32), ("reserved", ctypes.c_uint32 * 3)]
 
 
 class QLoraError(RuntimeError):
@@ -118,6 +141,25 @@ def load() -> ctypes.CDLL:
     lib.qlora_lrec_loss.argtypes = [vp] * 3 + [f32, f32] + [vp] * 4 + [c_int] * 3 + [vp, c_sz, vp]
     lib.qlora_lrec_loss_scaled.restype = c_int
     lib.qlora_lrec_loss_scaled.argtypes = [vp] * 3 + [f32, f32, f32] + [vp] * 4 + [c_int] * 3 + [vp, c_sz, vp]
+    i64, f64 = ctypes.c_int64, ctypes.c_double
+    lib.qlora_token_logprobs_workspace_bytes.restype = c_sz
+    lib.qlora_token_logprobs_workspace_bytes.argtypes = [c_int] * 4
+    lib.qlora_token_logprobs.restype = c_int
+    lib.qlora_token_logprobs.argtypes = [vp, i64] + [vp] * 5 + [c_int, vp] + [c_int] * 3 + [vp, c_sz, vp]
+    lib.qlora_token_logprobs_bwd.restype = c_int
+    lib.qlora_token_logprobs_bwd.argtypes = [vp, i64] + [vp] * 5 + [i64] + [c_int] * 3 + [vp]
+    lib.qlora_optim_plan_bytes.restype = c_sz
+    lib.qlora_optim_plan_bytes.argtypes = [c_int, vp]
+    lib.qlora_optim_plan.restype = c_int
+    lib.qlora_optim_plan.argtypes = [c_int, vp, vp, c_sz]
+    lib.qlora_optim_control_init.restype = c_int
+    lib.qlora_optim_control_init.argtypes = [vp, f32, f32, ctypes.c_uint32, ctypes.c_int32, f64, f64]
+    lib.qlora_optim_workspace_bytes.restype = c_sz
+    lib.qlora_optim_workspace_bytes.argtypes = []
+    lib.qlora_grad_norm.restype = c_int
+    lib.qlora_grad_norm.argtypes = [vp, vp, f32, vp, vp, c_sz, vp]
+    lib.qlora_adamw_step.restype = c_int
+    lib.qlora_adamw_step.argtypes = [vp] * 3 + [f64] * 4 + [vp, c_sz, vp]
     _lib = lib
     return lib
 
@@ -130,6 +172,15 @@ def _ptr(t) -> Optional[int]:
         return t
     if not t.is_contiguous():
         raise ValueError("qlora buffers must be contiguous")
+    return t.data_ptr()
+
+
+def _rows_ptr(t) -> Optional[int]:
+    """Pointer of a matrix whose rows may lie further apart than they are long (the call is handed the distance)."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.dim() > 0 and t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError("the entries of a row must be contiguous")
     return t.data_ptr()
 
 
@@ -484,4 +535,81 @@ def qlora_linear_bwd_dropout(dy, x, packed, scales, zeros, A, B, keep_mask, keep
                                          _ptr(workspace), workspace_bytes, _stream(stream))
     if check and st != 0:
         raise QLoraError(st, "qlora_linear_bwd_dropout")
+    return st
+
+
+def qlora_token_logprobs_workspace_bytes(M: int, V: int, alternatives: int, dtype: int) -> int:
+    return int(load().qlora_token_logprobs_workspace_bytes(M, V, alternatives, dtype))
+
+
+def qlora_token_logprobs(logits, row_stride: int, tokens, logprob, entropy, alt_tokens, alt_logprobs, alternatives: int,
+                         stats, M: int, V: int, dtype: int, workspace, workspace_bytes: Optional[int] = None,
+                         stream=None, check: bool = True) -> int:
+    if workspace_bytes is None:
+        workspace_bytes = _nbytes(workspace)
+    st = load().qlora_token_logprobs(_rows_ptr(logits), row_stride, _ptr(tokens), _ptr(logprob), _ptr(entropy),
+                                     _ptr(alt_tokens), _ptr(alt_logprobs), alternatives, _ptr(stats), M, V, dtype,
+                                     _ptr(workspace), workspace_bytes, _stream(stream))
+    if check and st != 0:
+        raise QLoraError(st, "qlora_token_logprobs")
+    return st
+
+
+def qlora_token_logprobs_bwd(logits, row_stride: int, tokens, stats, d_logprob, d_entropy, dlogits, d_row_stride: int,
+                             M: int, V: int, dtype: int, stream=None, check: bool = True) -> int:
+    st = load().qlora_token_logprobs_bwd(_rows_ptr(logits), row_stride, _ptr(tokens), _ptr(stats), _ptr(d_logprob),
+                                         _ptr(d_entropy), _rows_ptr(dlogits), d_row_stride, M, V, dtype, _stream(stream))
+    if check and st != 0:
+        raise QLoraError(st, "qlora_token_logprobs_bwd")
+    return st
+
+
+def qlora_optim_plan(tensors, check: bool = True):
+    """The plan of a list of OptimTensorStruct, as a ctypes buffer in host memory (with check=False: plan, status)."""
+    array = (OptimTensorStruct * len(tensors))(*tensors)
+    nbytes = int(load().qlora_optim_plan_bytes(len(tensors), array))
+    plan = ctypes.create_string_buffer(max(nbytes, 16))
+    st = load().qlora_optim_plan(len(tensors), array, plan, nbytes)
+    if check and st != 0:
+        raise QLoraError(st, "qlora_optim_plan")
+    return plan if check else (plan, st)
+
+
+def qlora_optim_plan_bytes(tensors) -> int:
+    return int(load().qlora_optim_plan_bytes(len(tensors), (OptimTensorStruct * len(tensors))(*tensors)))
+
+
+def qlora_optim_control_init(lr: float, grad_scale: float, seed: int, step: int, beta1: float, beta2: float,
+                             check: bool = True):
+    """A control block in host memory (with check=False: block, status)."""
+    control = OptimControlStruct()
+    st = load().qlora_optim_control_init(ctypes.byref(control), lr, grad_scale, seed, step, beta1, beta2)
+    if check and st != 0:
+        raise QLoraError(st, "qlora_optim_control_init")
+    return control if check else (control, st)
+
+
+def qlora_optim_workspace_bytes() -> int:
+    return int(load().qlora_optim_workspace_bytes())
+
+
+def qlora_grad_norm(plan, plan_device, grad_scale: float, norm, workspace, workspace_bytes: Optional[int] = None,
+                    stream=None, check: bool = True) -> int:
+    if workspace_bytes is None:
+        workspace_bytes = _nbytes(workspace)
+    st = load().qlora_grad_norm(plan, _ptr(plan_device), grad_scale, _ptr(norm), _ptr(workspace), workspace_bytes,
+                                _stream(stream))
+    if check and st != 0:
+        raise QLoraError(st, "qlora_grad_norm")
+    return st
+
+
+def qlora_adamw_step(plan, plan_device, control, beta1: float, beta2: float, eps: float, max_grad_norm: float, workspace,
+                     workspace_bytes: Optional[int] = None, stream=None, check: bool = True) -> int:
+    if workspace_bytes is None:
+        workspace_bytes = _nbytes(workspace)
+    st = load().qlora_adamw_step(plan, _ptr(plan_device), _ptr(control), beta1, beta2, eps, max_grad_norm,
+                                 _ptr(workspace), workspace_bytes, _stream(stream))
+    if check and st != 0:
+        raise QLoraError(st, "qlora_adamw_step")
     return st

@@ -7,7 +7,9 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <mutex>
+#include <new>
 #include <vector>
 
 using namespace qlora;
@@ -131,12 +133,14 @@ const char *qlora_status_string(int status)
     case QLORA_E_SHAPE: return "bad shape: need M >= 1, K % 32 == 0, N % 8 == 0 and sizes below 2^31 elements";
     case QLORA_E_GROUP: return "bad group size: need group_size % 32 == 0 and K % group_size == 0";
     case QLORA_E_RANK: return "rank must be 0 or a multiple of 8 up to 64";
-    case QLORA_E_DTYPE: return "dtype must be QLORA_F16 (0) or QLORA_BF16 (1)";
+    case QLORA_E_DTYPE: return "dtype must be QLORA_F16 (0) or QLORA_BF16 (1), or QLORA_F32 (2) where the call takes it";
     case QLORA_E_ALIGN: return "a pointer is not 16-byte aligned";
     case QLORA_E_WORKSPACE: return "workspace is NULL or smaller than qlora_workspace_bytes()";
     case QLORA_E_HIP: return "the HIP runtime reported an error";
     case QLORA_E_GIDX: return "group index out of range, or a group without exactly group_size columns";
     case QLORA_E_STATIC: return "the problem needs more scratch than the static device array holds: use qlora_linear_fwd with a workspace";
+    case QLORA_E_PLAN: return "not a plan of qlora_optim_plan, a plan without weights, or tensors that overlap";
+    case QLORA_E_VALUE: return "a number is out of its range";
     default: return "unknown status";
     }
 }
@@ -757,6 +761,260 @@ int qlora_lrec_loss_scaled(const void *student_logits, const void *teacher_logit
     begin_call();
     launch_lrec_loss(student_logits, teacher_logits, labels, lambda_kl, lambda_ce, grad_scale, kl, ce, (float *)workspace,
                      loss_mean, dlogits, M, V, dtype == QLORA_BF16, (hipStream_t)stream);
+    return end_call();
+}
+
+namespace {
+
+int check_logits(int M, int V, int dtype)
+{
+    if (M < 1 || V < 1 || M >= (1 << 22) || (long long)M * V >= (1ll << 35)) return QLORA_E_SHAPE;
+    if (dtype != QLORA_F16 && dtype != QLORA_BF16 && dtype != QLORA_F32) return QLORA_E_DTYPE;
+    return QLORA_OK;
+}
+int check_stride(int M, int V, int64_t stride)
+{
+    return stride < V || stride >= (1ll << 40) || stride * M >= (1ll << 40) ? QLORA_E_VALUE : QLORA_OK;
+}
+inline bool odd4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
+
+}  // namespace
+
+size_t qlora_token_logprobs_workspace_bytes(int M, int V, int alternatives, int dtype)
+{
+    if (check_logits(M, V, dtype) != QLORA_OK || alternatives < 0 || alternatives > QLORA_MAX_ALTERNATIVES) return 0;
+    const size_t bytes = score_workspace_bytes(M, V, alternatives, dtype);
+    return bytes ? round_up(bytes) : 0;
+}
+
+int qlora_token_logprobs(const void *logits, int64_t row_stride, const int32_t *tokens, float *logprob, float *entropy,
+                         int32_t *alt_tokens, float *alt_logprobs, int alternatives, float *stats, int M, int V,
+                         int dtype, void *workspace, size_t workspace_bytes, void *stream)
+{
+    int st = check_logits(M, V, dtype);
+    if (st != QLORA_OK) return st;
+    if ((st = check_stride(M, V, row_stride)) != QLORA_OK) return st;
+    if (alternatives < 0 || alternatives > QLORA_MAX_ALTERNATIVES) return QLORA_E_VALUE;
+    if (!logits || (logprob && !tokens) || (alternatives > 0 && (!alt_tokens || !alt_logprobs)) ||
+        (!logprob && !entropy && !stats && alternatives == 0))
+        return QLORA_E_NULL;
+    if (misaligned(logits) || misaligned(stats) || misaligned(workspace) || odd4(tokens) || odd4(logprob) || odd4(entropy) ||
+        (alternatives > 0 && (odd4(alt_tokens) || odd4(alt_logprobs))))
+        return QLORA_E_ALIGN;
+    const size_t need = qlora_token_logprobs_workspace_bytes(M, V, alternatives, dtype);
+    if (need && (!workspace || workspace_bytes < need)) return QLORA_E_WORKSPACE;
+    begin_call();
+    launch_token_logprobs(logits, row_stride, tokens, logprob, entropy, alt_tokens, alt_logprobs, alternatives, stats, M, V,
+                          dtype, workspace, (hipStream_t)stream);
+    return end_call();
+}
+
+int qlora_token_logprobs_bwd(const void *logits, int64_t row_stride, const int32_t *tokens, const float *stats,
+                             const float *d_logprob, const float *d_entropy, void *dlogits, int64_t d_row_stride, int M,
+                             int V, int dtype, void *stream)
+{
+    int st = check_logits(M, V, dtype);
+    if (st != QLORA_OK) return st;
+    if ((st = check_stride(M, V, row_stride)) != QLORA_OK || (st = check_stride(M, V, d_row_stride)) != QLORA_OK) return st;
+    if (dlogits == logits && d_row_stride != row_stride && M > 1) return QLORA_E_VALUE;
+    if (!logits || !stats || !dlogits || (!d_logprob && !d_entropy) || (d_logprob && !tokens)) return QLORA_E_NULL;
+    if (misaligned(logits) || misaligned(stats) || misaligned(dlogits) || odd4(tokens) || odd4(d_logprob) || odd4(d_entropy))
+        return QLORA_E_ALIGN;
+    begin_call();
+    launch_token_logprobs_bwd(logits, row_stride, tokens, stats, d_logprob, d_entropy, dlogits, d_row_stride, M, V, dtype,
+                              (hipStream_t)stream);
+    return end_call();
+}
+
+namespace {
+
+struct Range {
+    uintptr_t begin, end;
+    bool written;
+};
+
+inline bool beta_ok(double b) { return b >= 0.0 && b < 1.0; }
+inline size_t dtype_bytes(int dtype) { return dtype == QLORA_F32 ? 4 : 2; }
+
+// total weights, blocks and chunks of a set of tensors; false: a number out of range
+bool count_weights(int count, const qlora_optim_tensor_t *tensors, uint64_t &weights, uint64_t &blocks, uint64_t &chunks)
+{
+    weights = blocks = chunks = 0;
+    if (count < 1 || count > (1 << 20) || !tensors) return false;
+    for (int i = 0; i < count; ++i) {
+        const int64_t n = tensors[i].numel;
+        if (n < 0 || n > (1ll << 36)) return false;
+        weights += n;
+        blocks += (n + QLORA_OPTIM_BLOCK - 1) / QLORA_OPTIM_BLOCK;
+        chunks += (n + OPTIM_CHUNK - 1) / OPTIM_CHUNK;
+    }
+    // one workgroup of 256 threads a chunk, and fewer than 2^32 threads in a launch
+    return weights > 0 && chunks < (1u << 24);
+}
+
+int check_tensor(const qlora_optim_tensor_t &t)
+{
+    if (!t.grad) return QLORA_E_NULL;
+    if (t.grad_dtype < QLORA_F16 || t.grad_dtype > QLORA_F32) return QLORA_E_DTYPE;
+    if (misaligned(t.grad)) return QLORA_E_ALIGN;
+    if (!t.param) return QLORA_OK;
+    if (t.param_dtype < QLORA_F16 || t.param_dtype > QLORA_F32 || (t.master && t.param_dtype == QLORA_F32)) return QLORA_E_DTYPE;
+    if (t.state_bits != 8 && t.state_bits != 32) return QLORA_E_BITS;
+    if (!t.exp_avg || !t.exp_avg_sq || (t.state_bits == 8 && (!t.avg_scale || !t.avg_sq_scale))) return QLORA_E_NULL;
+    if (misaligned(t.param) || misaligned(t.master) || misaligned(t.exp_avg) || misaligned(t.exp_avg_sq) ||
+        (t.state_bits == 8 && (odd4(t.avg_scale) || odd4(t.avg_sq_scale))))
+        return QLORA_E_ALIGN;
+    if (!(t.lr_scale >= 0.f && t.lr_scale < INFINITY) || !(t.weight_decay >= 0.f && t.weight_decay < INFINITY))
+        return QLORA_E_VALUE;
+    return QLORA_OK;
+}
+
+// the buffers of a tensor, at most seven
+int ranges_of(const qlora_optim_tensor_t &t, Range *r)
+{
+    int n = 0;
+    const auto add = [&](const void *p, size_t bytes, bool written) {
+        if (p) r[n++] = Range{(uintptr_t)p, (uintptr_t)p + bytes, written};
+    };
+    const size_t numel = (size_t)t.numel, scales = (numel + QLORA_OPTIM_BLOCK - 1) / QLORA_OPTIM_BLOCK * 4;
+    add(t.grad, numel * dtype_bytes(t.grad_dtype), false);
+    if (t.param) {
+        add(t.param, numel * dtype_bytes(t.param_dtype), true);
+        add(t.master, numel * 4, true);
+        add(t.exp_avg, numel * t.state_bits / 8, true);
+        add(t.exp_avg_sq, numel * t.state_bits / 8, true);
+        if (t.state_bits == 8) {
+            add(t.avg_scale, scales, true);
+            add(t.avg_sq_scale, scales, true);
+        }
+    }
+    return n;
+}
+
+// the header of a plan in host memory, if it is one and its copy can be used
+int check_plan(const void *plan, const void *plan_device, OptimHeader &h)
+{
+    if (!plan || !plan_device) return QLORA_E_NULL;
+    if (misaligned(plan_device)) return QLORA_E_ALIGN;
+    std::copy_n((const char *)plan, sizeof h, (char *)&h);
+    return h.magic == OPTIM_MAGIC ? QLORA_OK : QLORA_E_PLAN;
+}
+
+}  // namespace
+
+size_t qlora_optim_plan_bytes(int count, const qlora_optim_tensor_t *tensors)
+{
+    uint64_t weights, blocks, chunks;
+    if (!count_weights(count, tensors, weights, blocks, chunks)) return 0;
+    return sizeof(OptimHeader) + sizeof(OptimTensor) * (size_t)count + 2 * sizeof(uint32_t) * (size_t)chunks;
+}
+
+int qlora_optim_plan(int count, const qlora_optim_tensor_t *tensors, void *plan, size_t plan_bytes)
+{
+    if (!tensors || !plan) return QLORA_E_NULL;
+    uint64_t weights, blocks, chunks;
+    if (!count_weights(count, tensors, weights, blocks, chunks)) return QLORA_E_SHAPE;
+    const size_t bytes = qlora_optim_plan_bytes(count, tensors);
+    if (plan_bytes < bytes) return QLORA_E_WORKSPACE;
+    bool steppable = true;
+    for (int i = 0; i < count; ++i) {
+        if (tensors[i].numel == 0) continue;
+        const int st = check_tensor(tensors[i]);
+        if (st != QLORA_OK) return st;
+        steppable = steppable && tensors[i].param;
+    }
+    {       // nothing that a step writes may be another buffer's
+        Range *all = new (std::nothrow) Range[(size_t)count * 7];
+        if (!all) return QLORA_E_WORKSPACE;
+        size_t n = 0;
+        for (int i = 0; i < count; ++i)
+            if (tensors[i].numel > 0) n += ranges_of(tensors[i], all + n);
+        std::sort(all, all + n, [](const Range &a, const Range &b) { return a.begin < b.begin; });
+        uintptr_t end = 0, written = 0;                    // furthest end so far, of all ranges and of the written ones
+        bool clash = false;
+        for (size_t i = 0; i < n && !clash; ++i) {
+            clash = all[i].begin < (all[i].written ? end : written);
+            end = std::max(end, all[i].end);
+            if (all[i].written) written = std::max(written, all[i].end);
+        }
+        delete[] all;
+        if (clash) return QLORA_E_PLAN;
+    }
+    OptimHeader h{};
+    h.magic = OPTIM_MAGIC;
+    h.bytes = bytes;
+    h.weights = weights;
+    h.count = (uint32_t)count;
+    h.chunks = (uint32_t)chunks;
+    h.steppable = steppable;
+    char *out = (char *)plan;
+    std::copy_n((const char *)&h, sizeof h, out);
+    out += sizeof h;
+    char *table = out + sizeof(OptimTensor) * (size_t)count;
+    uint32_t block = 0;
+    for (int i = 0; i < count; ++i) {
+        const qlora_optim_tensor_t &t = tensors[i];
+        const OptimTensor o{t.param, t.grad, t.master, t.exp_avg, t.exp_avg_sq, t.avg_scale, t.avg_sq_scale, t.numel, block,
+                            t.lr_scale, t.weight_decay, (uint8_t)t.param_dtype, (uint8_t)t.grad_dtype,
+                            (uint8_t)t.state_bits, 0};
+        std::copy_n((const char *)&o, sizeof o, out);
+        out += sizeof o;
+        block += (uint32_t)((t.numel + QLORA_OPTIM_BLOCK - 1) / QLORA_OPTIM_BLOCK);    // wraps: it only feeds a hash
+        const uint32_t n = (uint32_t)((t.numel + OPTIM_CHUNK - 1) / OPTIM_CHUNK);
+        for (uint32_t c = 0; c < n; ++c) {
+            const uint32_t entry[2] = {(uint32_t)i, c};
+            std::copy_n((const char *)entry, sizeof entry, table);
+            table += sizeof entry;
+        }
+    }
+    return QLORA_OK;
+}
+
+int qlora_optim_control_init(qlora_optim_control_t *control, float lr, float grad_scale, uint32_t seed, int32_t step,
+                             double beta1, double beta2)
+{
+    if (!control) return QLORA_E_NULL;
+    if (!beta_ok(beta1) || !beta_ok(beta2) || step < 0) return QLORA_E_VALUE;
+    qlora_optim_control_t c{};
+    c.lr = lr;
+    c.grad_scale = grad_scale;
+    c.seed = seed;
+    c.step = step;
+    c.beta1_power = std::pow(beta1, step);
+    c.beta2_power = std::pow(beta2, step);
+    *control = c;
+    return QLORA_OK;
+}
+
+size_t qlora_optim_workspace_bytes(void) { return round_up(sizeof(double) * OPTIM_PARTS); }
+
+int qlora_grad_norm(const void *plan, const void *plan_device, float grad_scale, float *norm, void *workspace,
+                    size_t workspace_bytes, void *stream)
+{
+    OptimHeader h;
+    const int st = check_plan(plan, plan_device, h);
+    if (st != QLORA_OK) return st;
+    if (!norm) return QLORA_E_NULL;
+    if (odd4(norm) || misaligned(workspace)) return QLORA_E_ALIGN;
+    if (!workspace || workspace_bytes < qlora_optim_workspace_bytes()) return QLORA_E_WORKSPACE;
+    begin_call();
+    launch_grad_norm(h, plan_device, grad_scale, norm, (double *)workspace, (hipStream_t)stream);
+    return end_call();
+}
+
+int qlora_adamw_step(const void *plan, const void *plan_device, qlora_optim_control_t *control, double beta1, double beta2,
+                     double eps, double max_grad_norm, void *workspace, size_t workspace_bytes, void *stream)
+{
+    OptimHeader h;
+    const int st = check_plan(plan, plan_device, h);
+    if (st != QLORA_OK) return st;
+    if (!h.steppable) return QLORA_E_PLAN;
+    if (!control) return QLORA_E_NULL;
+    if (!beta_ok(beta1) || !beta_ok(beta2) || !(eps >= 0.0 && eps < INFINITY) || !(max_grad_norm >= 0.0)) return QLORA_E_VALUE;
+    if (misaligned(control) || misaligned(workspace)) return QLORA_E_ALIGN;
+    if (max_grad_norm > 0.0 && (!workspace || workspace_bytes < qlora_optim_workspace_bytes())) return QLORA_E_WORKSPACE;
+    begin_call();
+    launch_adamw(h, plan_device, control, beta1, beta2, eps, max_grad_norm, (double *)workspace, (hipStream_t)stream);
     return end_call();
 }
 

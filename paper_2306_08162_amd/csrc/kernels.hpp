@@ -181,4 +181,51 @@ void launch_lrec_loss(const void *student, const void *teacher, const int32_t *l
                       float lambda_ce, float grad_scale, float *kl, float *ce, float *tok, float *loss_mean, void *grad,
                       int M, int V, bool bf16, hipStream_t s);
 
+// logprob.hip -- log probabilities of given tokens, entropy and top alternatives of rows of logits, and the gradient.
+// dt: 0 fp16, 1 bf16, 2 fp32.  A row is taken in `splits` segments of `seg` 16-byte pieces, one workgroup of `threads`
+// each; with more than one the workspace holds their results (score_workspace_bytes; 0 with one).
+struct ScorePlan {
+    int splits, seg, threads;
+};
+ScorePlan score_plan(int M, int V, int dt);
+size_t score_workspace_bytes(int M, int V, int k, int dt);
+// tokens, logprob, entropy, stats ([M,4]: maximum, sum of exp(z - maximum), its logarithm, entropy) may be NULL
+void launch_token_logprobs(const void *logits, long stride, const int32_t *tokens, float *logprob, float *entropy,
+                           int32_t *alt_tokens, float *alt_logprobs, int k, float *stats, int M, int V, int dt,
+                           void *workspace, hipStream_t s);
+void launch_token_logprobs_bwd(const void *logits, long stride, const int32_t *tokens, const float *stats,
+                               const float *d_logprob, const float *d_entropy, void *dlogits, long d_stride, int M, int V,
+                               int dt, hipStream_t s);
+
+// optim.hip -- AdamW over many tensors and the norm of their gradients.  A plan is a header, one record a tensor, and for
+// each chunk of OPTIM_CHUNK weights the tensor it belongs to and its number in there; the kernels read the copy in device
+// memory, the launchers the header alone.
+constexpr int OPTIM_CHUNK = 4096;
+constexpr unsigned OPTIM_PARTS = 1024;         // workgroups of the sum of squares, one partial sum each
+constexpr uint64_t OPTIM_MAGIC = 0x3170a4d4f5157ull;
+struct OptimHeader {
+    uint64_t magic, bytes, weights;
+    uint32_t count, chunks;
+    uint32_t steppable;                        // every tensor has weights and states
+    uint32_t reserved[7];
+};
+static_assert(sizeof(OptimHeader) == 64, "plan layout");
+struct OptimTensor {
+    void *param;
+    const void *grad;
+    float *master;                             // NULL: param itself is updated
+    void *exp_avg, *exp_avg_sq;
+    float *avg_scale, *avg_sq_scale;           // 8-bit states
+    int64_t numel;
+    uint32_t first_block;                      // blocks of weights of the tensors before it
+    float lr_scale, weight_decay;
+    uint8_t param_dtype, grad_dtype, state_bits, reserved;
+};
+static_assert(sizeof(OptimTensor) == 80, "plan layout");
+// parts: OPTIM_PARTS doubles
+void launch_grad_norm(const OptimHeader &h, const void *plan_device, float grad_scale, float *norm, double *parts,
+                      hipStream_t s);
+void launch_adamw(const OptimHeader &h, const void *plan_device, void *control, double beta1, double beta2, double eps,
+                  double max_norm, double *parts, hipStream_t s);
+
 }  // namespace qlora

@@ -5,7 +5,8 @@ C ABI the same way.  Nothing here computes anything.
 """
 from __future__ import annotations
 
-from typing import Optional
+from dataclasses import dataclass
+from typing import Optional, Sequence, Tuple
 
 import numpy as np
 import torch
@@ -308,3 +309,105 @@ class DeviceSiblings:
 
     def host_dx(self) -> np.ndarray:
         return _host16(self.dx)
+
+
+_FLAG = {torch.float16: ql.QLORA_F16, torch.bfloat16: ql.QLORA_BF16, torch.float32: ql.QLORA_F32}
+
+
+@dataclass
+class OptimTensor:
+    """One tensor of an AdapterOptimizer.  The dtypes are read off the tensors; for 16-bit patterns that travel as
+    int16 (as a DeviceLayer keeps them) they are given.  States that are None are allocated, as zeros."""
+
+    param: Optional[torch.Tensor]
+    grad: torch.Tensor
+    master: Optional[torch.Tensor] = None
+    exp_avg: Optional[torch.Tensor] = None
+    exp_avg_sq: Optional[torch.Tensor] = None
+    avg_scale: Optional[torch.Tensor] = None
+    avg_sq_scale: Optional[torch.Tensor] = None
+    lr_scale: float = 1.0
+    weight_decay: float = 0.0
+    param_dtype: Optional[int] = None
+    grad_dtype: Optional[int] = None
+    state_bits: Optional[int] = None            # None: 8 if exp_avg holds bytes, else 32
+
+
+class AdapterOptimizer:
+    """AdamW over the adapters of a model (and whatever is trained beside them): the plan, the control block and the
+    scratch of qlora_adamw_step and qlora_grad_norm.  The tensors keep their place in memory for its lifetime."""
+
+    def __init__(self, tensors: Sequence[OptimTensor], lr: float, betas: Tuple[float, float] = (0.9, 0.999),
+                 eps: float = 1e-8, max_grad_norm: float = 0.0, grad_scale: float = 1.0, seed: int = 0, step: int = 0):
+        self.tensors = list(tensors)
+        if not self.tensors:
+            raise ValueError("no tensors")
+        self.device = self.tensors[0].grad.device
+        self.betas, self.eps, self.max_grad_norm, self.grad_scale = tuple(betas), eps, max_grad_norm, grad_scale
+        self.plan = ql.qlora_optim_plan([self._describe(t) for t in self.tensors])
+        self.plan_device = self._upload(self.plan)
+        control = ql.qlora_optim_control_init(lr, grad_scale, seed, step, *self.betas)
+        self.control = self._upload(control)
+        self.workspace = torch.empty(ql.qlora_optim_workspace_bytes(), dtype=torch.uint8, device=self.device)
+        words = self.control.view(torch.float32)
+        self.lr, self.last_grad_norm = words[0:1], words[5:6]               # device floats: write lr, read the norm
+        self.device_grad_scale = words[1:2]
+        counts = self.control.view(torch.int32)
+        self.steps_taken, self.steps_skipped = counts[3:4], counts[4:5]
+
+    def _upload(self, host) -> torch.Tensor:
+        return torch.frombuffer(bytearray(host), dtype=torch.uint8).to(self.device)
+
+    def _describe(self, t: OptimTensor) -> ql.OptimTensorStruct:
+        n, s = t.grad.numel(), ql.OptimTensorStruct()
+        if t.state_bits is None:
+            t.state_bits = 8 if t.exp_avg is not None and t.exp_avg.element_size() == 1 else 32
+        if t.param is not None:
+            zeros = lambda size, dtype: torch.zeros(size, dtype=dtype, device=self.device)
+            state = torch.uint8 if t.state_bits == 8 else torch.float32
+            scales = -(-n // ql.OPTIM_BLOCK) if t.state_bits == 8 else 0
+            t.exp_avg = zeros(n, state) if t.exp_avg is None else t.exp_avg
+            t.exp_avg_sq = zeros(n, state) if t.exp_avg_sq is None else t.exp_avg_sq
+            if scales:
+                t.avg_scale = zeros(scales, torch.float32) if t.avg_scale is None else t.avg_scale
+                t.avg_sq_scale = zeros(scales, torch.float32) if t.avg_sq_scale is None else t.avg_sq_scale
+            # what the library takes by address alone: sizes and element sizes are checked here
+            width = 1 if t.state_bits == 8 else 4
+            for name, size, bytes_each in (("param", n, None), ("master", n, 4), ("exp_avg", n, width),
+                                           ("exp_avg_sq", n, width), ("avg_scale", scales, 4), ("avg_sq_scale", scales, 4)):
+                b = getattr(t, name)
+                if b is None or (name.endswith("scale") and not scales):
+                    continue
+                if b.numel() != size or (bytes_each and b.element_size() != bytes_each):
+                    raise ValueError(f"{name} of {b.numel()} x {b.element_size()} bytes beside a gradient of {n} entries")
+            s.param_dtype = _FLAG[t.param.dtype] if t.param_dtype is None else t.param_dtype
+            if t.param.element_size() != (4 if s.param_dtype == ql.QLORA_F32 else 2):
+                raise ValueError("param_dtype does not fit the tensor")
+            s.lr_scale, s.weight_decay, s.state_bits = t.lr_scale, t.weight_decay, t.state_bits
+        s.grad_dtype = _FLAG[t.grad.dtype] if t.grad_dtype is None else t.grad_dtype
+        if t.grad.element_size() != (4 if s.grad_dtype == ql.QLORA_F32 else 2):
+            raise ValueError("grad_dtype does not fit the tensor")
+        s.numel = n
+        for name in ("param", "grad", "master", "exp_avg", "exp_avg_sq", "avg_scale", "avg_sq_scale"):
+            b = getattr(t, name)
+            if b is None:
+                continue
+            if b.device != self.device:
+                raise ValueError("the tensors of a step live on one device")
+            setattr(s, name, ql._ptr(b))
+        return s
+
+    def _here(self):
+        if self.device.type == "cuda" and torch.cuda.current_device() != self.device.index:
+            raise ValueError(f"the tensors live on {self.device}, which is not the current device")
+
+    def step(self, stream=None) -> None:
+        self._here()
+        ql.qlora_adamw_step(self.plan, self.plan_device, self.control, self.betas[0], self.betas[1], self.eps,
+                            self.max_grad_norm, self.workspace, stream=stream)
+
+    def grad_norm(self, out: torch.Tensor, grad_scale: Optional[float] = None, stream=None) -> None:
+        """out [1] fp32: the norm of all gradients, times the grad_scale the optimizer was made with (or this one)."""
+        self._here()
+        ql.qlora_grad_norm(self.plan, self.plan_device, self.grad_scale if grad_scale is None else grad_scale, out,
+                           self.workspace, stream=stream)

@@ -1,0 +1,338 @@
+"""GPU parity of qlora_token_logprobs and its gradient against the fp64 oracle (oracle/scoring.py).
+
+Tolerances, by counting roundings (u = 2^-24).  A weight exp(z - m) carries one rounding of the difference, one of the
+product with log2 e (both relative to its exponent x, so |x| u each in the weight) and one unit of the hardware's exp2; a sum
+of a row passes at most 64 + 8 + 6 + 8 additions in a segment and 6 + a few more across segments.  So ln S is off
+by at most (100 + 2 E|x|) u, with E|x| <= H + ln S under the softmax, the difference z - m by u |z - m|, and
+    |logprob|: C u (1 + |z - m| + ln S),  |entropy|: C u (1 + H + ln S)  with C = 128
+covers them.  A gradient entry p (g + h (log p + H)) adds the relative error of p, (2 |x| + 100) u, and one rounding to the
+output type (half a unit in the last place, or half the smallest subnormal of fp16)."""
+import numpy as np
+import pytest
+
+import oracle
+from oracle import scoring
+from paper_2306_08162_amd import binding as ql
+from paper_2306_08162_amd import workloads as wl
+from parity import announce
+
+pytestmark = pytest.mark.gpu
+
+C, U = 128.0, 2.0 ** -24
+FLAG = {"f16": ql.QLORA_F16, "bf16": ql.QLORA_BF16, "f32": ql.QLORA_F32}
+HALF_ULP = {"f16": 2.0 ** -11, "bf16": 2.0 ** -8, "f32": 2.0 ** -24}
+TINY = {"f16": 2.0 ** -25, "bf16": 2.0 ** -126, "f32": 2.0 ** -126}
+
+
+def _torch(dtype):
+    import torch
+    return {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+
+
+def _logits(seed, M, V, dtype, spread=2.5):
+    """fp64 values that `dtype` holds exactly."""
+    z = wl.normal(seed, M * V).reshape(M, V) * spread
+    z[np.arange(M), (wl.splitmix64(seed + 1, 0, M) % np.uint64(V)).astype(np.int64)] += 12.0 * (np.arange(M) % 2)
+    return _rounded(z, dtype)
+
+
+def _rounded(z, dtype):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(z)).to(_torch(dtype)).double().numpy()
+
+
+def _upload(z, dtype, pad, fill=0.0):
+    import torch
+    M, V = z.shape
+    full = torch.full((M, V + pad), fill, dtype=_torch(dtype), device="cuda:0")
+    full[:, :V] = torch.from_numpy(np.ascontiguousarray(z)).to("cuda:0").to(_torch(dtype))
+    return full
+
+
+class _Call:
+    """Buffers of one problem, outputs filled with what no call writes."""
+
+    def __init__(self, z, tokens, dtype, k, pad=0, stats=True):
+        import torch
+        self.z, self.tokens_h, self.dtype, self.k, self.pad = z, np.asarray(tokens), dtype, k, pad
+        M, V = self.shape = z.shape
+        dev = "cuda:0"
+        self.logits = _upload(z, dtype, pad, 77.0)
+        self.tokens = torch.from_numpy(self.tokens_h.astype(np.int32)).to(dev)
+        new = lambda shape, t=torch.float32: torch.full(shape, 99, dtype=t, device=dev)
+        self.logprob, self.entropy, self.stats = new((M,)), new((M,)), new((M, 4)) if stats else None
+        self.alt = new((M, k), torch.int32) if k else None
+        self.alt_lp = new((M, k)) if k else None
+        nbytes = ql.qlora_token_logprobs_workspace_bytes(M, V, k, FLAG[dtype])
+        self.ws = torch.full((max(nbytes, 16),), 0xFF, dtype=torch.uint8, device=dev)
+
+    def forward(self, stream=None):
+        M, V = self.shape
+        ql.qlora_token_logprobs(self.logits, V + self.pad, self.tokens, self.logprob, self.entropy, self.alt, self.alt_lp,
+                                self.k, self.stats, M, V, FLAG[self.dtype], self.ws, stream=stream)
+
+    def check(self):
+        M, V = self.shape
+        lp, H, alt, alt_lp = scoring.score(self.z, self.tokens_h, self.k)
+        got = {n: getattr(self, n).double().cpu().numpy() for n in ("logprob", "entropy")}
+        with np.errstate(invalid="ignore"):
+            full = scoring.log_probabilities(self.z)
+            ls = np.nan_to_num(-(full.max(axis=1)), nan=0.0, posinf=0.0)           # ln S = -(log p of the largest)
+            given = (self.tokens_h >= 0) & (self.tokens_h < V)
+            d = np.abs(lp) + ls
+            self._near(got["logprob"], lp, C * U * (1 + np.nan_to_num(d, nan=0, posinf=0)))
+            self._near(got["entropy"], H, C * U * (1 + np.nan_to_num(H) + ls))
+            if self.k:
+                np.testing.assert_array_equal(self.alt.cpu().numpy(), alt)
+                far = np.nan_to_num(np.abs(alt_lp), nan=0, posinf=0) + ls[:, None]
+                self._near(self.alt_lp.double().cpu().numpy(), alt_lp, C * U * (1 + far))
+        return given
+
+    @staticmethod
+    def _near(got, want, bound):
+        np.testing.assert_array_equal(np.isnan(got), np.isnan(want))
+        inf = np.isinf(want)
+        np.testing.assert_array_equal(got[inf], want[inf])
+        ok = np.isfinite(want)
+        assert np.all(np.isfinite(got[ok])), "a finite value is expected"
+        worst = np.max(np.abs(got[ok] - want[ok]) / np.broadcast_to(bound, want.shape)[ok]) if ok.any() else 0.0
+        assert worst <= 1.0, f"{worst:.3g} times the bound"
+
+    def backward(self, g, h, d_pad=0, into=None, stream=None):
+        import torch
+        M, V = self.shape
+        up = lambda a: None if a is None else torch.from_numpy(np.asarray(a, np.float32)).to("cuda:0")
+        self.g, self.h = up(g), up(h)
+        self.dlogits = torch.full((M, V + d_pad), 55, dtype=_torch(self.dtype), device="cuda:0") if into is None else into
+        ql.qlora_token_logprobs_bwd(self.logits, V + self.pad, self.tokens, self.stats, self.g, self.h, self.dlogits,
+                                    self.dlogits.shape[1], M, V, FLAG[self.dtype], stream=stream)
+
+    def check_gradient(self):
+        M, V = self.shape
+        g = None if self.g is None else self.g.double().cpu().numpy()
+        h = None if self.h is None else self.h.double().cpu().numpy()
+        want = scoring.score_gradient(self.z, self.tokens_h, g, h)
+        got = self.dlogits[:, :V].double().cpu().numpy()
+        with np.errstate(invalid="ignore"):
+            lp = scoring.log_probabilities(self.z)
+            p = np.nan_to_num(np.exp(lp))
+            alp = np.nan_to_num(np.abs(lp), posinf=0, neginf=0)
+            H = (p * alp).sum(axis=1, keepdims=True)
+            ls = np.nan_to_num(-(lp.max(axis=1, keepdims=True)), nan=0, posinf=0)
+            zero = np.zeros((M, 1))
+            ga, ha = (zero if a is None else np.abs(a)[:, None] for a in (g, h))
+            slope = p * (ga + ha * (alp + H))
+            bound = C * U * (slope * (1 + alp + ls) + p * (ga + ha * (1 + H + ls)) + ga * (want != 0) * U)
+            bound += HALF_ULP[self.dtype] * 1.01 * np.nan_to_num(np.abs(want)) + TINY[self.dtype] * (1 + ga + ha)
+        self._near(got, want, bound)
+        if self.dlogits.shape[1] > V:
+            assert (self.dlogits[:, V:].float() == 55).all(), "entries behind the row were written"
+
+
+def _tokens(seed, M, V):
+    t = (wl.splitmix64(seed, 0, M) % np.uint64(V)).astype(np.int64)
+    t[M // 3::7] = -1
+    return t
+
+
+# V around every boundary: pieces of 8 (4 in fp32), 64 lanes, a workgroup's 64 KB, segments; V < k; rows at any alignment
+SHAPES = [
+    (3, 1, "f16", 5, 0), (2, 2, "f32", 1, 1), (3, 7, "bf16", 8, 1), (2, 8, "f16", 8, 3), (3, 9, "f32", 20, 0),
+    (4, 64, "bf16", 64, 0), (3, 65, "f16", 33, 7), (2, 511, "f32", 20, 2), (3, 513, "bf16", 5, 0), (2, 1025, "f16", 64, 5),
+    (2, 4096, "f16", 20, 0), (3, 4097, "f32", 5, 3), (2, 8200, "bf16", 40, 1), (5, 32000, "f16", 5, 0),
+    (2, 32003, "bf16", 20, 61), (2, 32768, "f16", 64, 0), (2, 32769, "f16", 20, 0), (3, 16384, "f32", 20, 0),
+    (2, 16385, "f32", 64, 0), (2, 50257, "f32", 8, 1), (2, 128259, "bf16", 20, 61), (1, 400001, "f16", 16, 0),
+    (70, 999, "f16", 3, 0), (33, 32000, "f32", 20, 0),
+]
+
+
+@pytest.mark.parametrize("M,V,dtype,k,pad", SHAPES)
+def test_scores_and_gradient(M, V, dtype, k, pad):
+    announce(f"token logprobs M={M} V={V} {dtype} k={k} pad={pad}")
+    c = _Call(_logits(V + M, M, V, dtype), _tokens(V, M, V), dtype, k, pad)
+    c.forward()
+    c.check()
+    g, h = wl.normal(V + 5, M) * 3.0, wl.normal(V + 6, M)
+    for gg, hh in ((g, h), (g, None), (None, h)):
+        c.backward(gg, hh, d_pad=pad % 5)
+        c.check_gradient()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("V", [100, 5000, 40000])
+def test_masks(V, dtype):
+    """Rows that mask all, all but one, all but a few, by -inf and by the type's lowest number; a masked target."""
+    announce(f"token logprobs masks V={V} {dtype}")
+    import torch
+    low = torch.finfo(_torch(dtype)).min
+    M = 10
+    z = _logits(V, M, V, dtype)
+    few = (wl.splitmix64(V + 9, 0, 6) % np.uint64(V)).astype(np.int64)
+    for row, fill in ((1, -np.inf), (2, -np.inf), (3, low), (4, low), (5, -np.inf), (6, low)):
+        keep = z[row].copy()
+        z[row] = fill
+        if row in (2, 4):
+            z[row, few[0]] = keep[few[0]]
+        if row in (5, 6):
+            z[row, few] = keep[few]
+    z[7, V // 2:] = -np.inf                      # half a row, and a target in it
+    z[8, ::3] = low
+    tokens = _tokens(V + 1, M, V)
+    tokens[:9] = [V, 0, few[0], 1, few[0], few[1], few[2], V - 1, 3]
+    for k in (8, 20, 64):
+        c = _Call(z, tokens, dtype, k)
+        c.forward()
+        c.check()
+    c.backward(np.linspace(-2, 2, M), np.linspace(1, -1, M))
+    c.check_gradient()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("kind", ["rising", "falling", "constant", "two_values", "hot_run", "integers", "zeros_of_both_signs"])
+def test_alternatives_of_rows_in_order(kind, dtype):
+    """Rows that defeat the first threshold: more entries above it than fit, and ties that go to the lower index."""
+    announce(f"token logprobs alternatives {kind} {dtype}")
+    M, V = 2, 20000
+    i = np.arange(V)
+    row = {"rising": i / 4096.0, "falling": -i / 4096.0, "constant": np.full(V, 1.5), "two_values": np.where(i % 7001 == 5, 2.0, 1.0),
+           "hot_run": np.where((i > 3000) & (i < 9000), 5.0 + (i % 997) / 512.0, -3.0),
+           "integers": (i * 7919 % 23).astype(float), "zeros_of_both_signs": np.where(i % 2 == 0, -0.0, 0.0)}[kind]
+    z = _rounded(np.stack([row, row[::-1]]), dtype)
+    for k in (1, 5, 8, 33, 64):
+        c = _Call(z, [3, V - 2], dtype, k)
+        c.forward()
+        c.check()
+
+
+@pytest.mark.parametrize("V", [50, 3000, 70000])
+def test_not_finite_rows(V):
+    """A NaN or plus infinity poisons its row and no other; rows whose gradients are 0 are zeros all the same."""
+    announce(f"token logprobs not finite V={V}")
+    z = _logits(3, 6, V, "f32")
+    z[1, V - 1] = np.nan
+    z[2, V // 2] = np.inf
+    z[4] = np.nan
+    z[5, 0], z[5, V - 1] = -np.inf, np.inf
+    c = _Call(z, [1, 2, V - 1, 0, 5, V - 1], "f32", 5)
+    c.forward()
+    c.check()
+    c.backward([1, 0, 2, 3, 0, 1], None)
+    got = c.dlogits.cpu().numpy()
+    assert (got[1] == 0).all() and (got[4] == 0).all()
+    assert np.isnan(got[2]).all() and np.isnan(got[5]).all()
+    want = scoring.score_gradient(z[[0, 3]], c.tokens_h[[0, 3]], np.array([1.0, 3.0]), None)
+    np.testing.assert_allclose(got[[0, 3]], want, rtol=1e-4, atol=1e-6)
+
+
+def test_almost_certain_tokens_keep_their_digits():
+    """log p = -s of a dominant token: relative accuracy where 1 + s would round s away."""
+    announce("token logprobs almost certain")
+    V = 32000
+    z = np.zeros((4, V))
+    for row, top in enumerate((20.0, 25.0, 30.0, 40.0)):
+        z[row, 100 * row] = top
+    c = _Call(z, [0, 100, 200, 300], "f32", 1)
+    c.forward()
+    lp, H, _, _ = scoring.score(z, c.tokens_h, 0)
+    # every weight is off by the same (2 * 40 * 1.45 + 2) u at most, the sum by 100 u, the entropy's factor by a few more
+    np.testing.assert_allclose(c.logprob.cpu().numpy(), lp, rtol=300 * U)
+    np.testing.assert_allclose(c.alt_lp.cpu().numpy()[:, 0], lp, rtol=300 * U)
+    np.testing.assert_allclose(c.entropy.cpu().numpy(), H, rtol=300 * U)
+
+
+def test_outputs_are_optional():
+    import torch
+    announce("token logprobs optional outputs")
+    M, V, k = 5, 40000, 7
+    z, tokens = _logits(8, M, V, "bf16"), _tokens(8, M, V)
+    full = _Call(z, tokens, "bf16", k)
+    full.forward()
+    names = ("logprob", "entropy", "alt", "stats")
+    for only in names:
+        c = _Call(z, tokens, "bf16", k if only == "alt" else 0)
+        for n in ("logprob", "entropy", "stats"):
+            if n != only:
+                setattr(c, n, None)
+        if only != "logprob":
+            c.tokens = None
+        c.forward()
+        assert torch.equal(getattr(c, only), getattr(full, only))
+        if only == "alt":
+            assert torch.equal(c.alt_lp, full.alt_lp)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_gradient_replaces_the_logits(dtype):
+    import torch
+    announce(f"token logprobs gradient in place {dtype}")
+    M, V = 4, 5003
+    c = _Call(_logits(12, M, V, dtype), _tokens(12, M, V), dtype, 0, pad=2)
+    c.forward()
+    g, h = np.linspace(1, 2, M), np.linspace(-1, 1, M)
+    c.backward(g, h)
+    apart = c.dlogits.clone()
+    c.backward(g, h, into=c.logits)
+    assert torch.equal(apart, c.logits[:, :V]) and (c.logits[:, V:].float() == 77).all()
+
+
+def test_results_repeat_and_follow_the_stream():
+    import torch
+    announce("token logprobs repeat, other stream")
+    M, V = 9, 50257
+    c = _Call(_logits(20, M, V, "f16"), _tokens(20, M, V), "f16", 20)
+    c.forward()
+    c.backward(np.ones(M), np.ones(M))
+    first = [t.clone() for t in (c.logprob, c.entropy, c.alt, c.alt_lp, c.stats, c.dlogits)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for t in (c.logprob, c.entropy, c.alt, c.alt_lp, c.stats, c.dlogits):
+        t.fill_(3)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        c.ws.fill_(0x7F)
+        c.forward()
+        c.backward(np.ones(M), np.ones(M))
+    side.synchronize()
+    for a, b in zip(first, (c.logprob, c.entropy, c.alt, c.alt_lp, c.stats, c.dlogits)):
+        assert torch.equal(a, b)
+
+
+def test_graph_replays_match_eager():
+    import torch
+    announce("token logprobs graph")
+    M, V = 6, 70001
+    c = _Call(_logits(30, M, V, "bf16"), _tokens(30, M, V), "bf16", 9)
+    others = [_upload(_logits(31 + i, M, V, "bf16"), "bf16", 0) for i in range(3)]
+    g = torch.ones(M, device="cuda:0")
+    d = torch.empty_like(c.logits)
+    flag = FLAG["bf16"]
+
+    def run():
+        c.forward()
+        ql.qlora_token_logprobs_bwd(c.logits, V, c.tokens, c.stats, g, g, d, V, M, V, flag)
+
+    outs = lambda: [t.clone() for t in (c.logprob, c.entropy, c.alt, c.alt_lp, c.stats, d)]
+    eager = []
+    for z in others:
+        c.logits.copy_(z)
+        run()
+        eager.append(outs())
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for rep in range(6):
+        c.logits.copy_(others[rep % 3])
+        for t in (c.logprob, c.entropy, c.alt, c.alt_lp, c.stats, d):
+            t.fill_(5)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(eager[rep % 3], outs()):
+            assert torch.equal(a, b), f"replay {rep}"
