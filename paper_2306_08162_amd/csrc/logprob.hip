@@ -13,11 +13,13 @@
 // the entries equal to the maximum as a count n apart from the sum s of all others, ln S = log1p(s) where n = 1, and
 // log p and H of such a row keep their relative accuracy.
 //
-// Alternatives.  The threads of a workgroup form g >= k groups; every group's largest entry is at least
-// tau = the smallest of the g maxima, so at least k entries are >= tau and, on rows in no special order, not many more
-// than g ln g: they are collected in LDS as 64-bit keys (value, lower index first) and sorted by waves.  Rows that break
-// the rule of thumb (an ordered vocabulary, masks of the type's lowest number) take exact detours: the threshold is
-// raised by bisection until the entries above it fit, and entries equal to it are taken in order of their index.
+// Alternatives.  Of its lanes' largest entries each of a workgroup's w waves finds (nearly) the ceil(k / w)-th, by bisection
+// with ballots; at least k entries are not below tau, the smallest of the w, and on rows in no special order not many more.
+// Those above tau are collected in LDS as 64-bit keys (value, lower index first), and a key's place among them is the number
+// of larger ones.  Rows that break the rule of thumb (an ordered vocabulary, masks of the type's lowest number) take exact
+// detours: the threshold is raised by bisection until the entries above it fit, and entries equal to it are taken in
+// order of their index.
+#include "../../include/qlora.h"
 #include "common.hpp"
 #include "kernels.hpp"
 
@@ -25,14 +27,14 @@ namespace qlora {
 
 namespace {
 
-constexpr int PT = 512;              // most threads of a workgroup
-constexpr int PCH = 8;               // 16-byte pieces a thread holds
-constexpr int PCAP = 1024;           // keys that LDS holds
+constexpr int PCAP = 512;            // keys that LDS holds
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 // x log2 of a weight that is zero: far below what exp2 can represent, and finite, so that 0 * x stays 0
 constexpr float NOTHING = -1024.f;
 
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+// max(x, NOTHING) for x <= a little above 0 (see max3 below for why not fmaxf)
+__device__ __forceinline__ float nothing_less(float x) { return __builtin_amdgcn_fmed3f(x, NOTHING, 1024.f); }
 
 struct ScoreArgs {
     const void *z;
@@ -51,6 +53,15 @@ struct ScoreArgs {
 // rows start at any element: 16-byte accesses with the alignment of an element
 typedef u32x4_t __attribute__((aligned(2))) loose_t;
 
+// The maximum that passes over NaN, in one instruction: fmaxf on bits just loaded costs the compiler another one for each
+// operand, to quiet a signalling NaN.
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
 // DT: 0 fp16, 1 bf16, 2 fp32
 template <int DT>
 struct Piece {
@@ -68,12 +79,11 @@ struct Piece {
             const half8_t h = __builtin_bit_cast(half8_t, w);
             const half2_t a = {h[0], h[1]}, b = {h[2], h[3]}, c = {h[4], h[5]}, d = {h[6], h[7]};
             const half2_t v = __builtin_elementwise_max(__builtin_elementwise_max(a, b), __builtin_elementwise_max(c, d));
-            return fmaxf((float)v[0], (float)v[1]);
+            return max3((float)v[0], (float)v[1], (float)v[1]);
+        } else if constexpr (DT == 1) {
+            return max3(max3(max3(val(0), val(1), val(2)), val(3), val(4)), max3(val(5), val(6), val(7)), val(7));
         } else {
-            float v = val(0);
-#pragma unroll
-            for (int e = 1; e < E; ++e) v = fmaxf(v, val(e));
-            return v;
+            return max3(max3(val(0), val(1), val(2)), val(3), val(3));
         }
     }
     // entries [0, have) of a row's last piece; the rest are -inf, which weighs nothing and is no alternative
@@ -95,6 +105,37 @@ struct Piece {
     }
 };
 
+// Lane 63 gathers its wave's values along rows of 16 lanes and from row to row (six steps without LDS), and hands the
+// result to all.  KEEP: what a lane without a partner combines with.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp(float keep, float v)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(keep), __float_as_int(v), CTRL, ROWS, 0xf, false));
+}
+template <typename F>
+__device__ __forceinline__ float wave_gather(float v, float keep, F f)
+{
+    v = f(v, dpp<0x111, 0xf>(keep, v));
+    v = f(v, dpp<0x112, 0xf>(keep, v));
+    v = f(v, dpp<0x114, 0xf>(keep, v));
+    v = f(v, dpp<0x118, 0xf>(keep, v));
+    v = f(v, dpp<0x142, 0xa>(keep, v));
+    v = f(v, dpp<0x143, 0xc>(keep, v));
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+__device__ __forceinline__ float wave_most(float v)
+{
+    return wave_gather(v, -INFINITY, [](float a, float b) { return max3(a, b, b); });
+}
+__device__ __forceinline__ float wave_least(float v)
+{
+    return -wave_gather(-v, -INFINITY, [](float a, float b) { return max3(a, b, b); });
+}
+__device__ __forceinline__ float wave_total(float v)
+{
+    return wave_gather(v, 0.f, [](float a, float b) { return a + b; });
+}
+
 // order of the floats as unsigned numbers (-0 counts as 0), and back
 __device__ __forceinline__ uint32_t order_of(float v)
 {
@@ -109,32 +150,6 @@ constexpr uint32_t ORDER_NINF = 0x007fffffu;           // order_of(-inf)
 
 typedef unsigned long long key_t;                      // order << 32 | ~index: larger is better, 0 is nothing
 
-__device__ __forceinline__ key_t shfl_key(key_t v, int from)
-{
-    const uint32_t lo = __shfl((uint32_t)v, from, WAVE), hi = __shfl((uint32_t)(v >> 32), from, WAVE);
-    return (key_t)hi << 32 | lo;
-}
-__device__ __forceinline__ key_t exchange(key_t v, int lane, int stride, bool descending)
-{
-    const key_t o = shfl_key(v, lane ^ stride);
-    return ((lane & stride) == 0) == descending ? (v > o ? v : o) : (v > o ? o : v);
-}
-// the wave's 64 keys in descending order over the lanes (bitonic)
-__device__ __forceinline__ key_t sort64(key_t v, int lane)
-{
-    for (int size = 2; size <= 64; size <<= 1)
-        for (int stride = size >> 1; stride > 0; stride >>= 1) v = exchange(v, lane, stride, (lane & size) == 0);
-    return v;
-}
-// the 64 largest of two descending lists
-__device__ __forceinline__ key_t merge64(key_t a, key_t b, int lane)
-{
-    const key_t r = shfl_key(b, 63 - lane);
-    a = a > r ? a : r;
-    for (int stride = 32; stride > 0; stride >>= 1) a = exchange(a, lane, stride, true);
-    return a;
-}
-
 // ln(n + s), with the accuracy of log1p where one entry is the maximum
 __device__ __forceinline__ float log_total(float n, float s) { return n == 1.f ? log1pf(s) : logf(n + s); }
 
@@ -147,20 +162,23 @@ __device__ __forceinline__ float logit_at(const void *row, long i)
         return cvt16<DT == 1>(((const uint16_t *)row)[i]);
 }
 
-// what a row's sums say: log p of the given token, entropy, statistics for the backward pass; one thread
+// the logit of the token given for a row; NaN and given = false: none
 template <int DT>
-__device__ __forceinline__ void write_row(const ScoreArgs &a, int row, const void *z, float m, float n, float s, float q,
-                                          float lt)
+__device__ __forceinline__ float given_logit(const ScoreArgs &a, int row, const void *z, bool &given)
+{
+    const int t = a.logprob ? a.token[row] : -1;
+    given = t >= 0 && t < a.V;
+    return given ? logit_at<DT>(z, t) : NAN;
+}
+
+// what a row's sums say: log p of the given token, entropy, statistics for the backward pass; one thread
+__device__ __forceinline__ void write_row(const ScoreArgs &a, int row, bool given, float zt, float m, float n, float s,
+                                          float q, float lt)
 {
     const bool empty = m == -INFINITY;
     const float total = n + s;
     const float h = empty ? 0.f : lt - LN2 * (q / total);
-    if (a.logprob) {
-        const int t = a.token[row];
-        float lp = 0.f;
-        if (t >= 0 && t < a.V) lp = empty ? -INFINITY : (logit_at<DT>(z, t) - m) - lt;
-        a.logprob[row] = lp;
-    }
+    if (a.logprob) a.logprob[row] = !given ? 0.f : empty ? -INFINITY : (zt - m) - lt;
     if (a.entropy) a.entropy[row] = h;
     if (a.stats) a.stats[row] = float4_t{empty ? 0.f : m, empty ? 1.f : total, lt, h};
 }
@@ -175,13 +193,26 @@ __device__ __forceinline__ void write_alternative(const ScoreArgs &a, int row, i
         poison ? NAN : none ? -INFINITY : (value_of((uint32_t)(key >> 32)) - m) - lt;
 }
 
-template <int DT>
+// piece i of the registers (a register has no address: i picks among them)
+template <int DT, int PCH>
+__device__ __forceinline__ Piece<DT> pick(const Piece<DT> *r, int i)
+{
+    Piece<DT> v = r[0];
+#pragma unroll
+    for (int j = 1; j < PCH; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v.w[e] = i == j ? r[j].w[e] : v.w[e];
+    return v;
+}
+
+// MOMENTS: the entropy is asked for, or the statistics that hold it.  At most PT threads with PCH pieces each.
+template <int DT, bool MOMENTS, int PT, int PCH>
 __global__ __launch_bounds__(PT) void score_kernel(const ScoreArgs a)
 {
     constexpr int E = Piece<DT>::E;
     __shared__ float red[5][PT / 64];                  // of each wave: maximum, smallest group maximum; n, s, q
     __shared__ int count, scan[PT / 64];
-    __shared__ key_t cand[PCAP], sorted[PT / 64][64];
+    __shared__ key_t cand[PCAP];
     const int T = blockDim.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = T >> 6;
     const int row = blockIdx.x / a.splits, split = blockIdx.x - row * a.splits;
     const int whole = a.V / E, rest = a.V - whole * E;                 // whole pieces of the row, entries of its last one
@@ -189,6 +220,9 @@ __global__ __launch_bounds__(PT) void score_kernel(const ScoreArgs a)
     const int p0 = split * a.seg, p1 = p0 + a.seg < pieces ? p0 + a.seg : pieces;
     const char *z = (const char *)a.z + (long)row * a.stride * (DT == 2 ? 4 : 2);
     if (tid == 0) count = 0;
+    bool given = false;
+    float zt = 0.f;
+    if (a.splits == 1 && wave == waves - 1) zt = given_logit<DT>(a, row, z, given);    // there when the sums are
 
     Piece<DT> r[PCH];
     float pm[PCH], mx = -INFINITY;
@@ -207,89 +241,102 @@ __global__ __launch_bounds__(PT) void score_kernel(const ScoreArgs a)
         pm[i] = r[i].max();
         mx = fmaxf(mx, pm[i]);
     }
-    // the wave's maximum and, for alternatives, the smallest maximum of its groups of `width` lanes: T / width >= k
-    float gm = mx;
-    {
-        int width = 64;
-        if (a.k > 0)
-            while (width > 1 && T / width < a.k) width >>= 1;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            mx = fmaxf(mx, __shfl_xor(mx, off, WAVE));
-            if (a.k > 0) {
-                const float o = __shfl_xor(gm, off, WAVE);
-                gm = off < width ? fmaxf(gm, o) : fminf(gm, o);
+    {       // the wave's maximum; for alternatives a bound that `rank` of its lanes' maxima reach
+        const float hi = wave_most(mx);
+        float bound = hi;
+        if (a.k > 0) {
+            const int rank = (a.k + waves - 1) / waves;
+            const uint32_t mine = order_of(mx);
+            uint32_t l = order_of(wave_least(mx)), h = order_of(hi);
+            for (int i = 0; i < 10 && h - l > 1; ++i) {                // rank lanes reach l
+                const uint32_t mid = l + (h - l) / 2;
+                if (__popcll(__ballot(mine >= mid)) >= rank)
+                    l = mid;
+                else
+                    h = mid;
             }
+            bound = value_of(l);
         }
         if (lane == 0) {
-            red[0][wave] = mx;
-            red[1][wave] = gm;
+            red[0][wave] = hi;
+            red[1][wave] = bound;
         }
     }
     __syncthreads();
-    float m = red[0][0], tau = red[1][0];
-    for (int w = 1; w < waves; ++w) {
-        m = fmaxf(m, red[0][w]);
-        tau = fminf(tau, red[1][w]);
-    }
+    const float m = wave_most(lane < waves ? red[0][lane] : -INFINITY);
+    const float tau = a.k > 0 ? wave_least(lane < waves ? red[1][lane] : INFINITY) : m;
 
-    // the sums: n entries equal to m, s = sum of exp(z - m) over the others, q = sum of exp(z - m) log2 exp(z - m)
-    const float base = m == -INFINITY ? 0.f : m;
+    // The sums: n entries equal to m, s = sum of w = exp(z - m) over the others, q = sum of w log2 w.  x = z log2 e - base with
+    // base = m log2 e rounded is one fused operation on the entry as it lies in the register; the rounding of base is the same
+    // factor 2^slip in every w, and is taken off at the end.  Pieces that hold the maximum are left out.
+    // Of a maximum so large that its product would leave the range, every other entry is so far away that its weight is zero by
+    // any factor.
+    const float factor = fabsf(m) < 0x1p126f ? LOG2E : 0.25f;
+    const float base = m == -INFINITY ? 0.f : m * factor;
+    const float slip = m == -INFINITY ? 0.f : fmaf(m, factor, -base);
     float n = 0.f, s = 0.f, q = 0.f;
-    const bool moments = a.entropy || a.stats;
+    uint32_t special = 0, highest = 0;                                 // pieces to look at again; those that hold the maximum
 #pragma unroll
     for (int i = 0; i < PCH; ++i) {
         if (p0 + i * T >= p1) break;
-        float ps = 0.f;
+        const bool apart = pm[i] == m;
+        highest |= apart ? 1u << i : 0u;
+        special |= apart || (a.k > 0 && pm[i] > tau) ? 1u << i : 0u;
+        float ps = 0.f, pq = 0.f;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const float x = (r[i].val(e) - base) * LOG2E;
+            const float x = fmaf(r[i].val(e), factor, -base);
             const float w = exp2_hw(x);
             ps += w;
-            if (moments) q = fmaf(w, fmaxf(x, NOTHING), q);
+            if constexpr (MOMENTS) pq = fmaf(w, nothing_less(x), pq);
         }
-        if (pm[i] == m || (a.k > 0 && pm[i] > tau)) {                  // few pieces: the maximum, and candidates
-            ps = 0.f;
+        s += apart ? 0.f : ps;
+        if constexpr (MOMENTS) q += apart ? 0.f : pq;
+    }
+    while (__any(special != 0)) {
+        if (special) {
+            const int i = __builtin_ctz(special);
+            special &= special - 1;
+            const Piece<DT> v8 = pick<DT, PCH>(r, i);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const float v = r[i].val(e);
-                if (v == m)
-                    n += 1.f;
-                else
-                    ps += exp2_hw((v - base) * LOG2E);
+                const float v = v8.val(e);
+                if (highest >> i & 1) {
+                    const float x = fmaf(v, factor, -base);
+                    const float w = v == m ? 0.f : exp2_hw(x);
+                    n += v == m ? 1.f : 0.f;
+                    s += w;
+                    if constexpr (MOMENTS) q = fmaf(w, nothing_less(x), q);
+                }
                 if (a.k > 0 && v > tau) {
                     const int at = atomicAdd(&count, 1);
                     if (at < PCAP) cand[at] = (key_t)order_of(v) << 32 | ~(uint32_t)((p0 + tid + i * T) * E + e);
                 }
             }
         }
-        s += ps;
     }
     if (m == -INFINITY) n = 0.f;                                       // every entry is masked (a NaN shows in s)
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) {
-        n += __shfl_xor(n, off, WAVE);
-        s += __shfl_xor(s, off, WAVE);
-        q += __shfl_xor(q, off, WAVE);
-    }
+    n = wave_total(n);
+    s = wave_total(s);
+    if constexpr (MOMENTS) q = wave_total(q);
     if (lane == 0) {
         red[2][wave] = n;
         red[3][wave] = s;
         red[4][wave] = q;
     }
     __syncthreads();
-    n = red[2][0], s = red[3][0], q = red[4][0];
-    for (int w = 1; w < waves; ++w) {
-        n += red[2][w];
-        s += red[3][w];
-        q += red[4][w];
-    }
+    n = wave_total(lane < waves ? red[2][lane] : 0.f);
+    s = wave_total(lane < waves ? red[3][lane] : 0.f);
+    if constexpr (MOMENTS) q = wave_total(lane < waves ? red[4][lane] : 0.f);
+    // w = 2^(x - slip): q = sum of w (x - slip)
+    q = (q - slip * s) * exp2_hw(-slip);
+    s *= exp2_hw(-slip);
     const bool poison = !(s < INFINITY) || m == INFINITY;
     const float lt = poison ? NAN : m == -INFINITY ? 0.f : log_total(n, s);
     if (a.splits > 1) {
         if (tid == 0) a.part[(long)row * a.splits + split] = float4_t{m, n, poison ? NAN : s, q};
-    } else if (tid == 0) {
-        write_row<DT>(a, row, z, poison ? NAN : m, n, s, poison ? NAN : q, lt);
+    } else if (tid == T - 64) {
+        write_row(a, row, given, zt, poison ? NAN : m, n, s, poison ? NAN : q, lt);
     }
     if (a.k == 0) return;
 
@@ -303,11 +350,11 @@ __global__ __launch_bounds__(PT) void score_kernel(const ScoreArgs a)
             if (tid == 0) count = 0;
             __syncthreads();
             int mine = 0;
+#pragma unroll 1
+            for (int i = 0; p0 + i * T < p1; ++i) {
+                const Piece<DT> v8 = pick<DT, PCH>(r, i);
 #pragma unroll
-            for (int i = 0; i < PCH; ++i) {
-                if (p0 + i * T >= p1) break;
-#pragma unroll
-                for (int e = 0; e < E; ++e) mine += order_of(r[i].val(e)) > t;
+                for (int e = 0; e < E; ++e) mine += order_of(v8.val(e)) > t;
             }
 #pragma unroll
             for (int off = 32; off > 0; off >>= 1) mine += __shfl_xor(mine, off, WAVE);
@@ -325,12 +372,12 @@ __global__ __launch_bounds__(PT) void score_kernel(const ScoreArgs a)
         __syncthreads();
         if (tid == 0) count = 0;
         __syncthreads();
-#pragma unroll
-        for (int i = 0; i < PCH; ++i) {
-            if (p0 + i * T >= p1) break;
+#pragma unroll 1
+        for (int i = 0; p0 + i * T < p1; ++i) {
+            const Piece<DT> v8 = pick<DT, PCH>(r, i);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const uint32_t o = order_of(r[i].val(e));
+                const uint32_t o = order_of(v8.val(e));
                 if (o > t) cand[atomicAdd(&count, 1)] = (key_t)o << 32 | ~(uint32_t)((p0 + tid + i * T) * E + e);
             }
         }
@@ -339,12 +386,12 @@ __global__ __launch_bounds__(PT) void score_kernel(const ScoreArgs a)
     }
     if (got < a.k && t > ORDER_NINF && !poison) {      // entries equal to t, lowest index first, until there are k
         int have = got;
-#pragma unroll
-        for (int i = 0; i < PCH; ++i) {
-            if (p0 + i * T >= p1 || have >= a.k) break;
+#pragma unroll 1
+        for (int i = 0; p0 + i * T < p1 && have < a.k; ++i) {
+            const Piece<DT> v8 = pick<DT, PCH>(r, i);
             int mine = 0;
 #pragma unroll
-            for (int e = 0; e < E; ++e) mine += order_of(r[i].val(e)) == t;
+            for (int e = 0; e < E; ++e) mine += order_of(v8.val(e)) == t;
             int upto = mine;
 #pragma unroll
             for (int off = 1; off < 64; off <<= 1) {
@@ -360,7 +407,7 @@ __global__ __launch_bounds__(PT) void score_kernel(const ScoreArgs a)
             }
 #pragma unroll
             for (int e = 0; e < E; ++e)
-                if (order_of(r[i].val(e)) == t) {
+                if (order_of(v8.val(e)) == t) {
                     if (at < a.k) cand[at] = (key_t)t << 32 | ~(uint32_t)((p0 + tid + i * T) * E + e);
                     ++at;
                 }
@@ -368,46 +415,50 @@ __global__ __launch_bounds__(PT) void score_kernel(const ScoreArgs a)
         }
         got = have < a.k ? have : a.k;
     }
-    // sorted by waves, 64 keys at a time, then joined by the first wave
-    const int chunks = (got + 63) / 64;
-    key_t best = 0;
-    for (int c = wave; c < chunks; c += waves) {
-        const int at = c * 64 + lane;
-        const key_t v = sort64(at < got ? cand[at] : 0, lane);
-        best = best == 0 && c == wave ? v : merge64(best, v, lane);
+    // a key's place is the number of larger ones; places beyond the last key hold nothing
+    for (int c = tid; c < got; c += T) {
+        const key_t mine = cand[c];
+        int place = 0;
+        for (int j = 0; j < got; ++j) place += cand[j] > mine;
+        if (place < a.k) {
+            if (a.splits > 1)
+                a.lists[((long)row * a.splits + split) * a.k + place] = mine;
+            else
+                write_alternative(a, row, place, mine, m, lt, poison);
+        }
     }
-    if (chunks > 1) {
-        sorted[wave][lane] = best;
-        __syncthreads();
+    for (int c = got + tid; c < a.k; c += T) {
+        if (a.splits > 1)
+            a.lists[((long)row * a.splits + split) * a.k + c] = 0;
+        else
+            write_alternative(a, row, c, 0, m, lt, poison);
     }
-    if (wave > 0) return;
-    for (int w = 1; w < waves && w < chunks; ++w) best = merge64(best, sorted[w][lane], lane);
-    if (lane >= a.k) return;
-    if (a.splits > 1)
-        a.lists[((long)row * a.splits + split) * a.k + lane] = best;
-    else
-        write_alternative(a, row, lane, best, m, lt, poison);
 }
 
 // joins the segments of a row; one wave a row
+constexpr int JOIN_KEYS = 256;
 template <int DT>
 __global__ __launch_bounds__(64) void score_join_kernel(const ScoreArgs a)
 {
+    __shared__ key_t keys[QLORA_MAX_ALTERNATIVES + JOIN_KEYS];         // the best so far, and the next lists' keys
     const int row = blockIdx.x, lane = threadIdx.x;
     const float4_t *part = a.part + (long)row * a.splits;
-    float m = -INFINITY;
-    bool bad = false;
-    for (int i = lane; i < a.splits; i += 64) {
+    bool given;
+    const float zt = given_logit<DT>(a, row, (const char *)a.z + (long)row * a.stride * (DT == 2 ? 4 : 2), given);
+    float4_t v = {-INFINITY, 0.f, 0.f, 0.f};
+    if (lane < a.splits) v = part[lane];
+    float m = v[0];
+    bool bad = v[2] != v[2];
+    for (int i = lane + 64; i < a.splits; i += 64) {
         m = fmaxf(m, part[i][0]);
         bad |= part[i][2] != part[i][2];
     }
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, WAVE));
+    m = wave_most(m);
     const bool poison = __any(bad);
     // a segment's sums, taken from its own maximum to the row's: exp(z - m) = f exp(z - mi), and its n entries join s
     float n = 0.f, s = 0.f, q = 0.f;
     for (int i = lane; i < a.splits; i += 64) {
-        const float4_t v = part[i];
+        if (i >= 64) v = part[i];
         if (v[0] == -INFINITY) continue;
         if (v[0] == m) {
             n += v[1];
@@ -419,20 +470,40 @@ __global__ __launch_bounds__(64) void score_join_kernel(const ScoreArgs a)
             q += f * fmaf(x, total, v[3]);
         }
     }
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) {
-        n += __shfl_xor(n, off, WAVE);
-        s += __shfl_xor(s, off, WAVE);
-        q += __shfl_xor(q, off, WAVE);
-    }
+    n = wave_total(n);
+    s = wave_total(s);
+    q = wave_total(q);
     const float lt = poison ? NAN : m == -INFINITY ? 0.f : log_total(n, s);
-    const char *z = (const char *)a.z + (long)row * a.stride * (DT == 2 ? 4 : 2);
-    if (lane == 0) write_row<DT>(a, row, z, poison ? NAN : m, n, s, poison ? NAN : q, lt);
+    if (lane == 0) write_row(a, row, given, zt, poison ? NAN : m, n, s, poison ? NAN : q, lt);
     if (a.k == 0) return;
     const key_t *lists = a.lists + (long)row * a.splits * a.k;
-    key_t best = lane < a.k ? lists[lane] : 0;
-    for (int i = 1; i < a.splits; ++i) best = merge64(best, lane < a.k ? lists[(long)i * a.k + lane] : 0, lane);
-    if (lane < a.k) write_alternative(a, row, lane, best, m, lt, poison);
+    const int all = a.splits * a.k;
+    int best = 0;                                                      // keys [0, best) are the best so far, in order
+    for (int at = 0; at < all; at += JOIN_KEYS) {
+        const int more = all - at < JOIN_KEYS ? all - at : JOIN_KEYS, have = best + more;
+        for (int i = lane; i < more; i += 64) keys[best + i] = lists[at + i];
+        __syncthreads();
+        key_t mine[(QLORA_MAX_ALTERNATIVES + JOIN_KEYS) / 64];
+        int place[(QLORA_MAX_ALTERNATIVES + JOIN_KEYS) / 64];
+#pragma unroll
+        for (int c = 0; c < (QLORA_MAX_ALTERNATIVES + JOIN_KEYS) / 64; ++c) {
+            const int i = lane + 64 * c;
+            mine[c] = i < have ? keys[i] : 0;
+            place[c] = mine[c] ? 0 : a.k;                              // key 0: a place that a short list left open
+            if (64 * c >= have) continue;
+            for (int j = 0; j < have; ++j) place[c] += keys[j] > mine[c];
+        }
+        __syncthreads();
+        int held = 0;
+#pragma unroll
+        for (int c = 0; c < (QLORA_MAX_ALTERNATIVES + JOIN_KEYS) / 64; ++c) {
+            if (place[c] < a.k) keys[place[c]] = mine[c];
+            held += __popcll(__ballot(place[c] < a.k));
+        }
+        best = held;
+        __syncthreads();
+    }
+    for (int i = lane; i < a.k; i += 64) write_alternative(a, row, i, i < best ? keys[i] : 0, m, lt, poison);
 }
 
 struct ScoreGradArgs {
@@ -510,12 +581,28 @@ __global__ __launch_bounds__(GT) void score_grad_kernel(const ScoreGradArgs a)
     }
 }
 
+// Many rows: 256 threads with 64 KB of a row, four workgroups on a compute unit.  Few: each has a compute unit to itself, and
+// 1024 threads get through it sooner.
+constexpr int MANY_PT = 256, MANY_PCH = 16, FEW_PT = 1024, FEW_PCH = 8;
+
 inline int pieces_of(int V, int dt) { return (int)(((long)V + (dt == 2 ? 3 : 7)) / (dt == 2 ? 4 : 8)); }
 
 template <int DT>
-void launch_score(const ScoreArgs &a, int threads, hipStream_t s)
+void launch_score(const ScoreArgs &a, const ScorePlan &p, hipStream_t s)
 {
-    QLORA_LAUNCH((score_kernel<DT>), dim3((unsigned)(a.M * a.splits)), dim3(threads), 0, s, a);
+    const dim3 grid((unsigned)(a.M * a.splits)), block(p.threads);
+    const bool moments = a.entropy || a.stats;
+    if (p.threads * FEW_PCH >= p.seg) {
+        if (moments)
+            QLORA_LAUNCH((score_kernel<DT, true, FEW_PT, FEW_PCH>), grid, block, 0, s, a);
+        else
+            QLORA_LAUNCH((score_kernel<DT, false, FEW_PT, FEW_PCH>), grid, block, 0, s, a);
+    } else {
+        if (moments)
+            QLORA_LAUNCH((score_kernel<DT, true, MANY_PT, MANY_PCH>), grid, block, 0, s, a);
+        else
+            QLORA_LAUNCH((score_kernel<DT, false, MANY_PT, MANY_PCH>), grid, block, 0, s, a);
+    }
     if (a.splits > 1) QLORA_LAUNCH((score_join_kernel<DT>), dim3(a.M), dim3(64), 0, s, a);
 }
 
@@ -525,11 +612,13 @@ ScorePlan score_plan(int M, int V, int dt)
 {
     const int pieces = pieces_of(V, dt);
     ScorePlan p;
-    p.splits = (pieces + PT * PCH - 1) / (PT * PCH);
+    p.splits = (pieces + MANY_PT * MANY_PCH - 1) / (MANY_PT * MANY_PCH);
+    const bool many = (long)M * p.splits > 256;
+    if (!many) p.splits = (pieces + FEW_PT * FEW_PCH - 1) / (FEW_PT * FEW_PCH);
     p.seg = (pieces + p.splits - 1) / p.splits;
+    const int most = many ? MANY_PT : FEW_PT;
     p.threads = 64;
-    while (p.threads < PT && p.threads * 2 < p.seg) p.threads *= 2;
-    while (p.threads * PCH < p.seg) p.threads *= 2;
+    while (p.threads < most && p.threads * 2 < p.seg) p.threads *= 2;
     return p;
 }
 
@@ -548,11 +637,11 @@ void launch_token_logprobs(const void *logits, long stride, const int32_t *token
     const ScoreArgs a{logits, stride, tokens, logprob, entropy, alt_tokens, alt_logprobs, (float4_t *)stats, M, V, k,
                       p.splits, p.seg, part, (key_t *)(part + (p.splits > 1 ? (size_t)M * p.splits : 0))};
     if (dt == 0)
-        launch_score<0>(a, p.threads, s);
+        launch_score<0>(a, p, s);
     else if (dt == 1)
-        launch_score<1>(a, p.threads, s);
+        launch_score<1>(a, p, s);
     else
-        launch_score<2>(a, p.threads, s);
+        launch_score<2>(a, p, s);
 }
 
 void launch_token_logprobs_bwd(const void *logits, long stride, const int32_t *tokens, const float *stats,
