@@ -86,22 +86,26 @@ struct Piece {
             return max3(max3(val(0), val(1), val(2)), val(3), val(3));
         }
     }
-    // entries [0, have) of a row's last piece; the rest are -inf, which weighs nothing and is no alternative
+    // -inf weighs nothing and is no alternative
+    __device__ __forceinline__ void clear()
+    {
+        constexpr uint32_t ninf = DT == 2 ? 0xff800000u : DT == 1 ? 0xff80ff80u : 0xfc00fc00u;
+        w = u32x4_t{ninf, ninf, ninf, ninf};
+    }
+    // entries [0, have) of a row's last piece, have < E
     __device__ __forceinline__ void load_part(const void *row, long at, int have)
     {
-        if constexpr (DT == 2) {
-            const uint32_t *p = (const uint32_t *)row + at;
+        clear();
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = e < have ? p[e] : 0xff800000u;
-        } else {
-            const uint16_t *p = (const uint16_t *)row + at;
-            constexpr uint32_t ninf = DT == 1 ? 0xff80u : 0xfc00u;
-#pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-                const uint32_t lo = e < have ? p[e] : ninf, hi = e + 1 < have ? p[e + 1] : ninf;
-                w[e >> 1] = lo | hi << 16;
+        for (int e = 0; e < E - 1; ++e)
+            if (e < have) {
+                if constexpr (DT == 2) {
+                    w[e] = ((const uint32_t *)row)[at + e];
+                } else {
+                    const uint32_t v = ((const uint16_t *)row)[at + e];
+                    w[e >> 1] = e & 1 ? (w[e >> 1] & 0xffffu) | v << 16 : (w[e >> 1] & 0xffff0000u) | v;
+                }
             }
-        }
     }
 };
 
@@ -136,6 +140,14 @@ __device__ __forceinline__ float wave_total(float v)
     return wave_gather(v, 0.f, [](float a, float b) { return a + b; });
 }
 
+// the sum over the eight lanes around a lane, all of them active
+__device__ __forceinline__ int sum8(int v)
+{
+    v += __builtin_amdgcn_mov_dpp(v, 0xB1, 0xf, 0xf, true);            // lane ^ 1
+    v += __builtin_amdgcn_mov_dpp(v, 0x4E, 0xf, 0xf, true);            // lane ^ 2
+    return v + __builtin_amdgcn_mov_dpp(v, 0x141, 0xf, 0xf, true);     // lane ^ 7: the other four's sum
+}
+
 // order of the floats as unsigned numbers (-0 counts as 0), and back
 __device__ __forceinline__ uint32_t order_of(float v)
 {
@@ -160,15 +172,6 @@ __device__ __forceinline__ float logit_at(const void *row, long i)
         return ((const float *)row)[i];
     else
         return cvt16<DT == 1>(((const uint16_t *)row)[i]);
-}
-
-// the logit of the token given for a row; NaN and given = false: none
-template <int DT>
-__device__ __forceinline__ float given_logit(const ScoreArgs &a, int row, const void *z, bool &given)
-{
-    const int t = a.logprob ? a.token[row] : -1;
-    given = t >= 0 && t < a.V;
-    return given ? logit_at<DT>(z, t) : NAN;
 }
 
 // what a row's sums say: log p of the given token, entropy, statistics for the backward pass; one thread
@@ -214,32 +217,45 @@ __global__ __launch_bounds__(PT) void score_kernel(const ScoreArgs a)
     __shared__ int count, scan[PT / 64];
     __shared__ key_t cand[PCAP];
     const int T = blockDim.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = T >> 6;
-    const int row = blockIdx.x / a.splits, split = blockIdx.x - row * a.splits;
+    const int row = blockIdx.x, split = blockIdx.y;
     const int whole = a.V / E, rest = a.V - whole * E;                 // whole pieces of the row, entries of its last one
     const int pieces = whole + (rest > 0);
     const int p0 = split * a.seg, p1 = p0 + a.seg < pieces ? p0 + a.seg : pieces;
     const char *z = (const char *)a.z + (long)row * a.stride * (DT == 2 ? 4 : 2);
+    const bool last_wave = wave == waves - 1;
     if (tid == 0) count = 0;
-    bool given = false;
-    float zt = 0.f;
-    if (a.splits == 1 && wave == waves - 1) zt = given_logit<DT>(a, row, z, given);    // there when the sums are
+    const int token = a.splits == 1 && last_wave && a.logprob ? a.token[row] : -1;
 
     Piece<DT> r[PCH];
     float pm[PCH], mx = -INFINITY;
+    const int full = (p1 < whole ? p1 : whole) - p0;                   // whole pieces of the segment
 #pragma unroll
     for (int i = 0; i < PCH; ++i) {
         if (p0 + i * T >= p1) break;
-        const int p = p0 + tid + i * T;
-        if (p < whole && p < p1)
-            r[i].w = *(const loose_t *)(z + 16 * (long)p);
-        else
-            r[i].load_part(z, (long)p * E, p == whole && p < p1 ? rest : 0);
+        const char *at = z + 16 * (long)(p0 + i * T);
+        if ((i + 1) * T <= full) {
+            r[i].w = *(const loose_t *)(at + 16u * (uint32_t)tid);
+        } else {
+            r[i].clear();
+            if (i * T + tid < full) r[i].w = *(const loose_t *)(at + 16u * (uint32_t)tid);
+        }
+    }
+    const bool given = token >= 0 && token < a.V;
+    const float zt = given ? logit_at<DT>(z, token) : NAN;             // on its way with the pieces
+    if (rest > 0 && p1 == pieces && ((whole - p0) & (T - 1)) == tid) { // the row's last, short piece
+        Piece<DT> last;
+        last.load_part(z, (long)whole * E, rest);
+        const int mine = (whole - p0) / T;
+#pragma unroll
+        for (int i = 0; i < PCH; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r[i].w[e] = mine == i ? last.w[e] : r[i].w[e];
     }
 #pragma unroll
     for (int i = 0; i < PCH; ++i) {
         if (p0 + i * T >= p1) break;
         pm[i] = r[i].max();
-        mx = fmaxf(mx, pm[i]);
+        mx = max3(mx, pm[i], pm[i]);
     }
     {       // the wave's maximum; for alternatives a bound that `rank` of its lanes' maxima reach
         const float hi = wave_most(mx);
@@ -248,14 +264,18 @@ __global__ __launch_bounds__(PT) void score_kernel(const ScoreArgs a)
             const int rank = (a.k + waves - 1) / waves;
             const uint32_t mine = order_of(mx);
             uint32_t l = order_of(wave_least(mx)), h = order_of(hi);
-            for (int i = 0; i < 10 && h - l > 1; ++i) {                // rank lanes reach l
+            int reach = rank == 1 ? 1 : 64;                            // so many lanes reach l
+            for (int i = 0; i < 12 && reach > rank + rank / 4 && h - l > 1; ++i) {
                 const uint32_t mid = l + (h - l) / 2;
-                if (__popcll(__ballot(mine >= mid)) >= rank)
+                const int above = __popcll(__ballot(mine >= mid));
+                if (above >= rank) {
                     l = mid;
-                else
+                    reach = above;
+                } else {
                     h = mid;
+                }
             }
-            bound = value_of(l);
+            bound = rank == 1 ? hi : value_of(l);
         }
         if (lane == 0) {
             red[0][wave] = hi;
@@ -275,13 +295,11 @@ __global__ __launch_bounds__(PT) void score_kernel(const ScoreArgs a)
     const float base = m == -INFINITY ? 0.f : m * factor;
     const float slip = m == -INFINITY ? 0.f : fmaf(m, factor, -base);
     float n = 0.f, s = 0.f, q = 0.f;
+    const float low = a.k > 0 ? tau : m;
     uint32_t special = 0, highest = 0;                                 // pieces to look at again; those that hold the maximum
 #pragma unroll
     for (int i = 0; i < PCH; ++i) {
         if (p0 + i * T >= p1) break;
-        const bool apart = pm[i] == m;
-        highest |= apart ? 1u << i : 0u;
-        special |= apart || (a.k > 0 && pm[i] > tau) ? 1u << i : 0u;
         float ps = 0.f, pq = 0.f;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
@@ -290,8 +308,15 @@ __global__ __launch_bounds__(PT) void score_kernel(const ScoreArgs a)
             ps += w;
             if constexpr (MOMENTS) pq = fmaf(w, nothing_less(x), pq);
         }
-        s += apart ? 0.f : ps;
-        if constexpr (MOMENTS) q += apart ? 0.f : pq;
+        if (__any(pm[i] >= low)) {
+            const bool apart = pm[i] == m;
+            highest |= apart ? 1u << i : 0u;
+            special |= apart || pm[i] > low ? 1u << i : 0u;
+            ps = apart ? 0.f : ps;
+            pq = apart ? 0.f : pq;
+        }
+        s += ps;
+        if constexpr (MOMENTS) q += pq;
     }
     while (__any(special != 0)) {
         if (special) {
@@ -332,7 +357,8 @@ __global__ __launch_bounds__(PT) void score_kernel(const ScoreArgs a)
     q = (q - slip * s) * exp2_hw(-slip);
     s *= exp2_hw(-slip);
     const bool poison = !(s < INFINITY) || m == INFINITY;
-    const float lt = poison ? NAN : m == -INFINITY ? 0.f : log_total(n, s);
+    float lt = 0.f;
+    if (a.k > 0 || last_wave) lt = poison ? NAN : m == -INFINITY ? 0.f : log_total(n, s);
     if (a.splits > 1) {
         if (tid == 0) a.part[(long)row * a.splits + split] = float4_t{m, n, poison ? NAN : s, q};
     } else if (tid == T - 64) {
@@ -415,12 +441,14 @@ __global__ __launch_bounds__(PT) void score_kernel(const ScoreArgs a)
         }
         got = have < a.k ? have : a.k;
     }
-    // a key's place is the number of larger ones; places beyond the last key hold nothing
-    for (int c = tid; c < got; c += T) {
+    // a key's place is the number of larger ones, counted by eight lanes; places beyond the last key hold nothing
+    for (int c = tid >> 3; c < got; c += T >> 3) {
         const key_t mine = cand[c];
         int place = 0;
-        for (int j = 0; j < got; ++j) place += cand[j] > mine;
-        if (place < a.k) {
+#pragma unroll 4
+        for (int j = tid & 7; j < got; j += 8) place += cand[j] > mine;
+        place = sum8(place);
+        if ((tid & 7) == 0 && place < a.k) {
             if (a.splits > 1)
                 a.lists[((long)row * a.splits + split) * a.k + place] = mine;
             else
@@ -443,8 +471,9 @@ __global__ __launch_bounds__(64) void score_join_kernel(const ScoreArgs a)
     __shared__ key_t keys[QLORA_MAX_ALTERNATIVES + JOIN_KEYS];         // the best so far, and the next lists' keys
     const int row = blockIdx.x, lane = threadIdx.x;
     const float4_t *part = a.part + (long)row * a.splits;
-    bool given;
-    const float zt = given_logit<DT>(a, row, (const char *)a.z + (long)row * a.stride * (DT == 2 ? 4 : 2), given);
+    const int token = a.logprob ? a.token[row] : -1;
+    const bool given = token >= 0 && token < a.V;
+    const float zt = given ? logit_at<DT>((const char *)a.z + (long)row * a.stride * (DT == 2 ? 4 : 2), token) : NAN;
     float4_t v = {-INFINITY, 0.f, 0.f, 0.f};
     if (lane < a.splits) v = part[lane];
     float m = v[0];
@@ -490,8 +519,12 @@ __global__ __launch_bounds__(64) void score_join_kernel(const ScoreArgs a)
             const int i = lane + 64 * c;
             mine[c] = i < have ? keys[i] : 0;
             place[c] = mine[c] ? 0 : a.k;                              // key 0: a place that a short list left open
-            if (64 * c >= have) continue;
-            for (int j = 0; j < have; ++j) place[c] += keys[j] > mine[c];
+        }
+#pragma unroll 4
+        for (int j = 0; j < have; ++j) {
+            const key_t other = keys[j];
+#pragma unroll
+            for (int c = 0; c < (QLORA_MAX_ALTERNATIVES + JOIN_KEYS) / 64; ++c) place[c] += other > mine[c];
         }
         __syncthreads();
         int held = 0;
@@ -537,10 +570,9 @@ __global__ __launch_bounds__(GT) void score_grad_kernel(const ScoreGradArgs a)
 #pragma unroll
         for (int i = 0; i < GCH; ++i) {
             const int p = p0 + i * GT;
-            if (p < whole)
-                r[i].w = *(const loose_t *)(z + 16 * (long)p);
-            else
-                r[i].load_part(z, (long)p * E, p == whole ? rest : 0);
+            r[i].clear();
+            if (p < whole) r[i].w = *(const loose_t *)(z + 16 * (long)p);
+            else if (p == whole && rest > 0) r[i].load_part(z, (long)p * E, rest);
         }
     }
 #pragma unroll
@@ -590,7 +622,7 @@ inline int pieces_of(int V, int dt) { return (int)(((long)V + (dt == 2 ? 3 : 7))
 template <int DT>
 void launch_score(const ScoreArgs &a, const ScorePlan &p, hipStream_t s)
 {
-    const dim3 grid((unsigned)(a.M * a.splits)), block(p.threads);
+    const dim3 grid(a.M, a.splits), block(p.threads);
     const bool moments = a.entropy || a.stats;
     if (p.threads * FEW_PCH >= p.seg) {
         if (moments)
@@ -616,9 +648,13 @@ ScorePlan score_plan(int M, int V, int dt)
     const bool many = (long)M * p.splits > 256;
     if (!many) p.splits = (pieces + FEW_PT * FEW_PCH - 1) / (FEW_PT * FEW_PCH);
     p.seg = (pieces + p.splits - 1) / p.splits;
-    const int most = many ? MANY_PT : FEW_PT;
     p.threads = 64;
-    while (p.threads < most && p.threads * 2 < p.seg) p.threads *= 2;
+    if (many) {     // what a wave does once a row weighs more than its pieces: few waves, as long as the chip has sixteen a unit
+        while (p.threads * MANY_PCH < p.seg) p.threads *= 2;
+        while (p.threads < MANY_PT && p.threads * 2 < p.seg && (long)M * p.splits * p.threads < 256 * 1024) p.threads *= 2;
+    } else {
+        while (p.threads < FEW_PT && p.threads * 2 < p.seg) p.threads *= 2;
+    }
     return p;
 }
 
