@@ -214,8 +214,10 @@ __global__ __launch_bounds__(PT) void score_kernel(const ScoreArgs a)
 {
     constexpr int E = Piece<DT>::E;
     __shared__ float red[5][PT / 64];                  // of each wave: maximum, smallest group maximum; n, s, q
-    __shared__ int count, scan[PT / 64];
-    __shared__ key_t cand[PCAP];
+    __shared__ int hits, count, scan[PT / 64];
+    __shared__ u32x4_t held[PCAP];                     // pieces with an entry above tau, and which they are
+    __shared__ int held_at[PCAP];
+    __shared__ key_t cand[PCAP];                       // entries above tau
     const int T = blockDim.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = T >> 6;
     const int row = blockIdx.x, split = blockIdx.y;
     const int whole = a.V / E, rest = a.V - whole * E;                 // whole pieces of the row, entries of its last one
@@ -223,7 +225,7 @@ __global__ __launch_bounds__(PT) void score_kernel(const ScoreArgs a)
     const int p0 = split * a.seg, p1 = p0 + a.seg < pieces ? p0 + a.seg : pieces;
     const char *z = (const char *)a.z + (long)row * a.stride * (DT == 2 ? 4 : 2);
     const bool last_wave = wave == waves - 1;
-    if (tid == 0) count = 0;
+    if (tid == 0) hits = count = 0;
     const int token = a.splits == 1 && last_wave && a.logprob ? a.token[row] : -1;
 
     Piece<DT> r[PCH];
@@ -296,49 +298,39 @@ __global__ __launch_bounds__(PT) void score_kernel(const ScoreArgs a)
     const float slip = m == -INFINITY ? 0.f : fmaf(m, factor, -base);
     float n = 0.f, s = 0.f, q = 0.f;
     const float low = a.k > 0 ? tau : m;
-    uint32_t special = 0, highest = 0;                                 // pieces to look at again; those that hold the maximum
 #pragma unroll
     for (int i = 0; i < PCH; ++i) {
         if (p0 + i * T >= p1) break;
-        float ps = 0.f, pq = 0.f;
+        float x[E], w[E], ps = 0.f, pq = 0.f;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const float x = fmaf(r[i].val(e), factor, -base);
-            const float w = exp2_hw(x);
-            ps += w;
-            if constexpr (MOMENTS) pq = fmaf(w, nothing_less(x), pq);
+            x[e] = fmaf(r[i].val(e), factor, -base);
+            w[e] = exp2_hw(x[e]);
+            ps += w[e];
+            if constexpr (MOMENTS) pq = fmaf(w[e], nothing_less(x[e]), pq);
         }
         if (__any(pm[i] >= low)) {
-            const bool apart = pm[i] == m;
-            highest |= apart ? 1u << i : 0u;
-            special |= apart || pm[i] > low ? 1u << i : 0u;
-            ps = apart ? 0.f : ps;
-            pq = apart ? 0.f : pq;
-        }
-        s += ps;
-        if constexpr (MOMENTS) q += pq;
-    }
-    while (__any(special != 0)) {
-        if (special) {
-            const int i = __builtin_ctz(special);
-            special &= special - 1;
-            const Piece<DT> v8 = pick<DT, PCH>(r, i);
+            if (pm[i] == m) {
+                ps = pq = 0.f;
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float v = v8.val(e);
-                if (highest >> i & 1) {
-                    const float x = fmaf(v, factor, -base);
-                    const float w = v == m ? 0.f : exp2_hw(x);
-                    n += v == m ? 1.f : 0.f;
-                    s += w;
-                    if constexpr (MOMENTS) q = fmaf(w, nothing_less(x), q);
+                for (int e = 0; e < E; ++e) {
+                    const bool top = r[i].val(e) == m;
+                    n += top ? 1.f : 0.f;
+                    w[e] = top ? 0.f : w[e];
+                    ps += w[e];
+                    if constexpr (MOMENTS) pq = fmaf(w[e], nothing_less(x[e]), pq);
                 }
-                if (a.k > 0 && v > tau) {
-                    const int at = atomicAdd(&count, 1);
-                    if (at < PCAP) cand[at] = (key_t)order_of(v) << 32 | ~(uint32_t)((p0 + tid + i * T) * E + e);
+            }
+            if (a.k > 0 && pm[i] > tau) {
+                const int at = atomicAdd(&hits, 1);
+                if (at < PCAP) {
+                    held[at] = r[i].w;
+                    held_at[at] = p0 + tid + i * T;
                 }
             }
         }
+        s += ps;
+        if constexpr (MOMENTS) q += pq;
     }
     if (m == -INFINITY) n = 0.f;                                       // every entry is masked (a NaN shows in s)
     n = wave_total(n);
@@ -366,10 +358,22 @@ __global__ __launch_bounds__(PT) void score_kernel(const ScoreArgs a)
     }
     if (a.k == 0) return;
 
-    int got = poison ? 0 : count;
-    uint32_t t = order_of(tau);                                        // entries above t are in the list
-    if (got > PCAP) {                                                  // too many: raise t
-        uint32_t lo = t, hi = order_of(m);                             // more than PCAP above lo, none above hi
+    const int pieces_held = poison ? 0 : hits;
+    uint32_t t = order_of(tau);                                        // entries above t are to be in the list
+    if (pieces_held <= PCAP) {
+        for (int j = tid; j < pieces_held * E; j += T) {
+            const float v = logit_at<DT>(held, j);
+            if (v > tau) {
+                const int at = atomicAdd(&count, 1);
+                if (at < PCAP) cand[at] = (key_t)order_of(v) << 32 | ~(uint32_t)(held_at[j / E] * E + j % E);
+            }
+        }
+        __syncthreads();
+    }
+    int got = count;
+    if (pieces_held > PCAP || got > PCAP) {                            // too many: raise t
+        uint32_t lo = t, hi = order_of(m);                             // more than PCAP or k above lo, none above hi
+        got = PCAP + 1;
         while (hi - lo > 1) {
             t = lo + (hi - lo) / 2;
             __syncthreads();
@@ -613,9 +617,9 @@ __global__ __launch_bounds__(GT) void score_grad_kernel(const ScoreGradArgs a)
     }
 }
 
-// Many rows: 256 threads with 64 KB of a row, four workgroups on a compute unit.  Few: each has a compute unit to itself, and
-// 1024 threads get through it sooner.
-constexpr int MANY_PT = 256, MANY_PCH = 16, FEW_PT = 1024, FEW_PCH = 8;
+// Many rows: 256 threads with 64 KB of a row, four workgroups on a compute unit (or 512 with 128 KB, where that spares the
+// second launch).  Few: each has a compute unit to itself, and 1024 threads get through it sooner.
+constexpr int MANY_PT = 512, MANY_PCH = 16, FEW_PT = 1024, FEW_PCH = 8, SEGMENT = 4096;
 
 inline int pieces_of(int V, int dt) { return (int)(((long)V + (dt == 2 ? 3 : 7)) / (dt == 2 ? 4 : 8)); }
 
@@ -644,14 +648,14 @@ ScorePlan score_plan(int M, int V, int dt)
 {
     const int pieces = pieces_of(V, dt);
     ScorePlan p;
-    p.splits = (pieces + MANY_PT * MANY_PCH - 1) / (MANY_PT * MANY_PCH);
+    p.splits = pieces <= MANY_PT * MANY_PCH ? 1 : (pieces + SEGMENT - 1) / SEGMENT;
     const bool many = (long)M * p.splits > 256;
     if (!many) p.splits = (pieces + FEW_PT * FEW_PCH - 1) / (FEW_PT * FEW_PCH);
     p.seg = (pieces + p.splits - 1) / p.splits;
     p.threads = 64;
     if (many) {     // what a wave does once a row weighs more than its pieces: few waves, as long as the chip has sixteen a unit
         while (p.threads * MANY_PCH < p.seg) p.threads *= 2;
-        while (p.threads < MANY_PT && p.threads * 2 < p.seg && (long)M * p.splits * p.threads < 256 * 1024) p.threads *= 2;
+        while (p.threads < 256 && p.threads * 2 < p.seg && (long)M * p.splits * p.threads < 256 * 1024) p.threads *= 2;
     } else {
         while (p.threads < FEW_PT && p.threads * 2 < p.seg) p.threads *= 2;
     }
