@@ -40,26 +40,40 @@ __device__ __forceinline__ uint32_t mix(uint32_t x)
     return x ^ (x >> 16);
 }
 
-// four consecutive entries as they lie in memory: fp32 in four words, 16-bit in two; `have` of them exist, the rest are 0
-__device__ __forceinline__ u32x4_t load4(const void *p, long i, int dtype, long have)
+// Device memory by type: a pointer read from the plan would otherwise be taken for one into any memory, with slower loads.
+template <typename T>
+__device__ __forceinline__ T load_global(const void *p, uint32_t byte)
+{
+    typedef const T __attribute__((address_space(1))) global_t;
+    return *(global_t *)((uintptr_t)p + byte);
+}
+template <typename T>
+__device__ __forceinline__ void store_global(void *p, uint32_t byte, T v)
+{
+    typedef T __attribute__((address_space(1))) global_t;
+    *(global_t *)((uintptr_t)p + byte) = v;
+}
+
+// Entries [i, i + 4) of a chunk that begins at p and has `have` of them (FULL: all of CHUNK), as they lie in memory: fp32 in
+// four words, 16-bit ones in two; those that do not exist are 0 and are not stored.
+template <bool FULL>
+__device__ __forceinline__ u32x4_t load4(const void *p, uint32_t i, int dtype, uint32_t have)
 {
     u32x4_t r = {0, 0, 0, 0};
     if (dtype == QLORA_F32) {
-        const uint32_t *f = (const uint32_t *)p + i;
-        if (have >= 4)
-            r = *(const u32x4_t *)f;
+        if (FULL || i + 4 <= have)
+            r = load_global<u32x4_t>(p, 4 * i);
         else
-            for (int e = 0; e < 3; ++e)
-                if (e < have) r[e] = f[e];
+            for (uint32_t e = 0; e < 3; ++e)
+                if (i + e < have) r[e] = load_global<uint32_t>(p, 4 * (i + e));
     } else {
-        const uint16_t *h = (const uint16_t *)p + i;
-        if (have >= 4) {
-            const u32x2_t v = *(const u32x2_t *)h;
+        if (FULL || i + 4 <= have) {
+            const u32x2_t v = load_global<u32x2_t>(p, 2 * i);
             r[0] = v[0];
             r[1] = v[1];
         } else
-            for (int e = 0; e < 3; ++e)
-                if (e < have) r[e >> 1] |= (uint32_t)h[e] << (16 * (e & 1));
+            for (uint32_t e = 0; e < 3; ++e)
+                if (i + e < have) r[e >> 1] |= (uint32_t)load_global<uint16_t>(p, 2 * (i + e)) << (16 * (e & 1));
     }
     return r;
 }
@@ -76,45 +90,47 @@ __device__ __forceinline__ void widen4(const u32x4_t &r, int dtype, float *f)
         for (int e = 0; e < 4; ++e) f[e] = f16_bits_to_f32((uint16_t)(r[e >> 1] >> (16 * (e & 1))));
     }
 }
-__device__ __forceinline__ void store4(void *p, long i, int dtype, long have, const float *f)
+template <bool FULL>
+__device__ __forceinline__ void store4(void *p, uint32_t i, int dtype, uint32_t have, const float *f)
 {
     if (dtype == QLORA_F32) {
-        float *d = (float *)p + i;
-        if (have >= 4)
-            *(float4_t *)d = float4_t{f[0], f[1], f[2], f[3]};
+        if (FULL || i + 4 <= have)
+            store_global(p, 4 * i, float4_t{f[0], f[1], f[2], f[3]});
         else
-            for (int e = 0; e < 3; ++e)
-                if (e < have) d[e] = f[e];
+            for (uint32_t e = 0; e < 3; ++e)
+                if (i + e < have) store_global(p, 4 * (i + e), f[e]);
     } else {
-        uint16_t *d = (uint16_t *)p + i;
         u16x4_t h;
 #pragma unroll
         for (int e = 0; e < 4; ++e) h[e] = dtype == QLORA_BF16 ? f32_to_bf16_bits(f[e]) : f32_to_f16_bits(f[e]);
-        if (have >= 4)
-            *(u16x4_t *)d = h;
+        if (FULL || i + 4 <= have)
+            store_global(p, 2 * i, h);
         else
-            for (int e = 0; e < 3; ++e)
-                if (e < have) d[e] = h[e];
+            for (uint32_t e = 0; e < 3; ++e)
+                if (i + e < have) store_global(p, 2 * (i + e), (uint16_t)h[e]);
     }
 }
-__device__ __forceinline__ uint32_t load_codes(const void *p, long i, long have)
+template <bool FULL>
+__device__ __forceinline__ uint32_t load_codes(const void *p, uint32_t i, uint32_t have)
 {
-    const uint8_t *c = (const uint8_t *)p + i;
-    if (have >= 4) return *(const uint32_t *)c;
+    if (FULL || i + 4 <= have) return load_global<uint32_t>(p, i);
     uint32_t r = 0;
-    for (int e = 0; e < 3; ++e)
-        if (e < have) r |= (uint32_t)c[e] << (8 * e);
+    for (uint32_t e = 0; e < 3; ++e)
+        if (i + e < have) r |= (uint32_t)load_global<uint8_t>(p, i + e) << (8 * e);
     return r;
 }
-__device__ __forceinline__ void store_codes(void *p, long i, long have, uint32_t r)
+template <bool FULL>
+__device__ __forceinline__ void store_codes(void *p, uint32_t i, uint32_t have, uint32_t r)
 {
-    uint8_t *c = (uint8_t *)p + i;
-    if (have >= 4)
-        *(uint32_t *)c = r;
+    if (FULL || i + 4 <= have)
+        store_global(p, i, r);
     else
-        for (int e = 0; e < 3; ++e)
-            if (e < have) c[e] = (uint8_t)(r >> (8 * e));
+        for (uint32_t e = 0; e < 3; ++e)
+            if (i + e < have) store_global(p, i + e, (uint8_t)(r >> (8 * e)));
 }
+__device__ __forceinline__ uint32_t size_of(int dtype) { return dtype == QLORA_F32 ? 4 : 2; }
+__device__ __forceinline__ void *advance(const void *p, uint64_t bytes) { return (char *)p + bytes; }
+
 __device__ __forceinline__ void decode4(uint32_t codes, float scale, float *f)
 {
     const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, true);
@@ -124,23 +140,56 @@ __device__ __forceinline__ void decode4(uint32_t codes, float scale, float *f)
     f[3] = hi[1] * scale;
 }
 
-// largest of the wave's values, as unsigned numbers (for bits of floats >= 0 the order of the floats; NaN above all)
+// largest of the wave's values, as unsigned numbers (for bits of floats >= 0 the order of the floats; NaN above all): lane 63
+// gathers it along rows of 16 lanes and from row to row
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t max_dpp(uint32_t v)
+{
+    const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
+    return v > o ? v : o;
+}
 __device__ __forceinline__ uint32_t wave_max_bits(uint32_t v)
 {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) {
-        const uint32_t o = __shfl_xor(v, off, WAVE);
-        v = v > o ? v : o;
+    v = max_dpp<0x111, 0xf>(v);
+    v = max_dpp<0x112, 0xf>(v);
+    v = max_dpp<0x114, 0xf>(v);
+    v = max_dpp<0x118, 0xf>(v);
+    v = max_dpp<0x142, 0xa>(v);
+    v = max_dpp<0x143, 0xc>(v);
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+
+// The smallest k >= -126 with x <= 1.75 * 2^k for the float x > 0 of these bits: its exponent, one more where the mantissa
+// exceeds 0x600000.
+__device__ __forceinline__ int scale_of(uint32_t bits)
+{
+    const int k = (int)((bits + 0x1fffffu) >> 23) - 127;
+    return k > -126 ? k : -126;
+}
+// The smallest k with x <= (1.75 * 2^k)^2 = 3.0625 * 4^k: half of the exponent, rounded down, after one more where the
+// mantissa exceeds 0x440000 (1.53125; of an even exponent that changes nothing).
+__device__ __forceinline__ int root_scale_of(uint32_t bits)
+{
+    int b = (int)bits;
+    if (b < 0x00800000) {                      // a number below the smallest normal one: as if there were exponents below 0
+        const int top = 31 - __builtin_clz(bits | 1u);
+        b = (b << (23 - top)) - 0x00800000 + (top - 22) * 0x00800000;
     }
-    return v;
+    return ((((b + 0x3bffff) >> 23) - 127) >> 1);
 }
 
 // |x| <= 1.75 * 2^k, 0 <= r < 2^20: the e4m3 code of x / 2^(k - 8), rounded up where r exceeds the distance.  Multiplied by 2^-112
 // (k taken off first) the code's exponent and mantissa are the top bits of the float, below the smallest normal code too.
 __device__ __forceinline__ uint32_t encode(float x, int k, uint32_t r)
 {
-    const float y = fminf(ldexpf(fabsf(x), -112 - k), 1.75f * 0x1p-112f);
-    return ((__float_as_uint(y) + r) >> 20) | (__float_as_uint(x) >> 31) << 7;
+    const uint32_t y = __float_as_uint(ldexpf(fabsf(x), -112 - k));
+    return ((y + r) >> 20) | (__float_as_uint(x) >> 24 & 0x80u);
+}
+// the same for x >= 0 that is a hardware square root: it may lie one unit above 1.75 * 2^k
+__device__ __forceinline__ uint32_t encode_root(float x, int k, uint32_t r)
+{
+    const uint32_t y = __float_as_uint(fminf(ldexpf(x, -112 - k), 1.75f * 0x1p-112f));
+    return (y + r) >> 20;
 }
 
 // the sum of the partial sums, the same in every thread of every workgroup
@@ -174,19 +223,39 @@ __global__ __launch_bounds__(OT) void grad_square_kernel(const OptimTensor *__re
                                                          double beta2)
 {
     if (control && blockIdx.x == 0 && threadIdx.x == 0) prepare_step(control, beta1, beta2);
-    double s = 0.0;
-    for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
+    // whose chunk is next is found out while this one's gradients are on their way
+    struct Place {
+        const void *grad;
+        uint32_t have;
+        int dtype;
+    };
+    const auto place = [&](uint32_t c) {
         const u32x2_t at = table[c];
         const OptimTensor *t = tensors + at[0];
-        const int dtype = t->grad_dtype;
-        const long first = (long)at[1] * CHUNK + threadIdx.x * 4, n = t->numel;
+        const long left = t->numel - (long)at[1] * CHUNK;
+        return Place{advance(t->grad, (uint64_t)at[1] * CHUNK * size_of(t->grad_dtype)),
+                     (uint32_t)(left < CHUNK ? left : CHUNK), t->grad_dtype};
+    };
+    double s = 0.0;
+    uint32_t c = blockIdx.x;
+    Place next = place(c);
+    while (c < chunks) {
+        const Place now = next;
         u32x4_t g[PASSES];
+        if (now.have == CHUNK) {
 #pragma unroll
-        for (int i = 0; i < PASSES; ++i) g[i] = load4(t->grad, first + i * OT * 4, dtype, n - first - i * OT * 4);
+            for (int i = 0; i < PASSES; ++i) g[i] = load4<true>(now.grad, (i * OT + threadIdx.x) * 4, now.dtype, CHUNK);
+        } else {
+#pragma unroll
+            for (int i = 0; i < PASSES; ++i)
+                g[i] = load4<false>(now.grad, (i * OT + threadIdx.x) * 4, now.dtype, now.have);
+        }
+        c += gridDim.x;
+        if (c < chunks) next = place(c);
 #pragma unroll
         for (int i = 0; i < PASSES; ++i) {
             float f[4];
-            widen4(g[i], dtype, f);
+            widen4(g[i], now.dtype, f);
 #pragma unroll
             for (int e = 0; e < 4; ++e) s = fma((double)f[e], (double)f[e], s);
         }
@@ -234,33 +303,43 @@ __device__ __forceinline__ void adam4(const AdamArgs &a, const AdamCoef &c, cons
     }
 }
 
-template <int BITS>
+template <int BITS, bool FULL>
 __device__ __forceinline__ void step_chunk(const AdamArgs &a, const OptimTensor &t, uint32_t chunk)
 {
-    const long first = (long)chunk * CHUNK + threadIdx.x * 4, n = t.numel;
+    const uint64_t begin = (uint64_t)chunk * CHUNK;
+    const long left = t.numel - (long)begin;
+    const uint32_t have = FULL ? CHUNK : (uint32_t)(left < CHUNK ? left : CHUNK);
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const bool master = t.master != nullptr;
-    const int wide = master ? (int)QLORA_F32 : t.param_dtype;
-    const void *wp = master ? (const void *)t.master : t.param;
+    const int wide = master ? (int)QLORA_F32 : t.param_dtype, grad_dtype = t.grad_dtype, param_dtype = t.param_dtype;
+    constexpr int SBYTES = BITS / 8;
+    const void *grad = advance(t.grad, begin * size_of(grad_dtype));
+    void *param = advance(t.param, begin * size_of(param_dtype)), *main = master ? advance(t.master, begin * 4) : param;
+    void *avg = advance(t.exp_avg, begin * SBYTES), *avg_sq = advance(t.exp_avg_sq, begin * SBYTES);
+    void *avg_scale = advance(t.avg_scale, begin / QBLOCK * 4), *avg_sq_scale = advance(t.avg_sq_scale, begin / QBLOCK * 4);
     u32x4_t g[PASSES], w[PASSES], m[PASSES], v[PASSES];
     float ms[PASSES], vs[PASSES];
 #pragma unroll
     for (int i = 0; i < PASSES; ++i) {
-        const long at = first + i * OT * 4, have = n - at;
-        g[i] = load4(t.grad, at, t.grad_dtype, have);
-        w[i] = load4(wp, at, wide, have);
+        const uint32_t at = (i * OT + threadIdx.x) * 4;
+        g[i] = load4<FULL>(grad, at, grad_dtype, have);
+        w[i] = load4<FULL>(main, at, wide, have);
         if constexpr (BITS == 32) {
-            m[i] = load4(t.exp_avg, at, QLORA_F32, have);
-            v[i] = load4(t.exp_avg_sq, at, QLORA_F32, have);
+            m[i] = load4<FULL>(avg, at, QLORA_F32, have);
+            v[i] = load4<FULL>(avg_sq, at, QLORA_F32, have);
         } else {
-            m[i][0] = load_codes(t.exp_avg, at, have);
-            v[i][0] = load_codes(t.exp_avg_sq, at, have);
-            const long block = (at - (threadIdx.x & 63) * 4) / QBLOCK;         // the wave's
-            ms[i] = block * QBLOCK < n ? t.avg_scale[block] : 0.f;
-            vs[i] = block * QBLOCK < n ? t.avg_sq_scale[block] : 0.f;
+            const uint32_t block = i * (OT / 64) + wave;               // the wave's
+            const bool some = FULL || block * QBLOCK < have;
+            m[i][0] = load_codes<FULL>(avg, at, have);
+            v[i][0] = load_codes<FULL>(avg_sq, at, have);
+            ms[i] = some ? load_global<float>(avg_scale, 4 * block) : 0.f;
+            vs[i] = some ? load_global<float>(avg_sq_scale, 4 * block) : 0.f;
         }
     }
     const qlora_optim_control_t *ctl = a.control;
     float gscale = ctl->grad_scale;
+    const float lr = ctl->lr, rate = ctl->rate * t.lr_scale, root = ctl->root;
+    const uint32_t key = ctl->key + (t.first_block + (uint32_t)(begin / QBLOCK)) * QBLOCK + lane * 4;
     if (a.count > 0) {
         const double norm = sqrt(sum_parts(a.parts, a.count)) * fabs((double)gscale);
         const bool finite = (float)norm < INFINITY;
@@ -268,16 +347,16 @@ __device__ __forceinline__ void step_chunk(const AdamArgs &a, const OptimTensor 
             a.control->grad_norm = (float)norm;
             if (!finite) a.control->skipped += 1;
         }
-        if (!finite) return;                                                   // the step is not taken
+        if (!finite) return;                                           // the step is not taken
         const double clip = a.max_norm / norm;
-        gscale *= (float)(clip < 1.0 ? clip : 1.0);                            // (norm 0: no gradient to clip)
+        gscale *= (float)(clip < 1.0 ? clip : 1.0);                    // (norm 0: no gradient to clip)
     }
-    const AdamCoef c{gscale, 1.f - ctl->lr * t.lr_scale * t.weight_decay, ctl->rate * t.lr_scale, ctl->root};
+    const AdamCoef c{gscale, 1.f - lr * t.lr_scale * t.weight_decay, rate, root};
 #pragma unroll
     for (int i = 0; i < PASSES; ++i) {
-        const long at = first + i * OT * 4, have = n - at;
+        const uint32_t at = (i * OT + threadIdx.x) * 4;
         float gf[4], wf[4], mf[4], vf[4], uf[4];
-        widen4(g[i], t.grad_dtype, gf);
+        widen4(g[i], grad_dtype, gf);
         widen4(w[i], wide, wf);
         if constexpr (BITS == 32) {
             widen4(m[i], QLORA_F32, mf);
@@ -290,10 +369,8 @@ __device__ __forceinline__ void step_chunk(const AdamArgs &a, const OptimTensor 
         }
         adam4(a, c, gf, mf, vf, uf, wf);
         if constexpr (BITS == 32) {
-            if (have > 0) {
-                store4(t.exp_avg, at, QLORA_F32, have, mf);
-                store4(t.exp_avg_sq, at, QLORA_F32, have, vf);
-            }
+            store4<FULL>(avg, at, QLORA_F32, have, mf);
+            store4<FULL>(avg_sq, at, QLORA_F32, have, vf);
         } else {
             uint32_t mb = 0, vb = 0;
 #pragma unroll
@@ -304,37 +381,25 @@ __device__ __forceinline__ void step_chunk(const AdamArgs &a, const OptimTensor 
             }
             mb = wave_max_bits(mb);
             vb = wave_max_bits(vb);
-            // 2^k: the largest |m| is at most 1.75 * 2^k, the largest v at most (1.75 * 2^k)^2 = 3.0625 * 4^k
-            int km, kv;
-            const float mf1 = frexpf(__uint_as_float(mb), &km);
-            km = max(km - 1 + (mf1 > 0.875f), -126);
-            const float vmax = __uint_as_float(vb);
-            frexpf(vmax, &kv);
-            kv = (kv - 1) >> 1;
-            kv += ldexpf(vmax, -2 * kv) > 3.0625f;
-            const long block = (at - (threadIdx.x & 63) * 4) / QBLOCK;
-            const uint32_t place = (t.first_block + (uint32_t)block) * QBLOCK + (threadIdx.x & 63) * 4 + ctl->key;
+            const int km = scale_of(mb), kv = root_scale_of(vb);
+            const uint32_t block = i * (OT / 64) + wave;
             uint32_t mc = 0, vc = 0;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const uint32_t r = mix(place + e);
+                const uint32_t r = mix(key + block * QBLOCK + e);
                 mc |= encode(mf[e], km, r >> 12) << (8 * e);
-                const uint32_t q = encode(uf[e], kv, r & 0xfffffu);
+                const uint32_t q = encode_root(uf[e], kv, r & 0xfffffu);
                 vc |= (q == 0 && vf[e] > 0.f ? 1u : q) << (8 * e);
             }
-            if (have > 0) {
-                store_codes(t.exp_avg, at, have, mc);
-                store_codes(t.exp_avg_sq, at, have, vc);
-                if ((threadIdx.x & 63) == 0) {     // an infinity or a NaN makes NaN of the whole block
-                    t.avg_scale[block] = mb == 0 ? 0.f : mb >= 0x7f800000u ? NAN : ldexpf(1.f, km - 8);
-                    t.avg_sq_scale[block] = vb == 0 ? 0.f : vb >= 0x7f800000u ? NAN : ldexpf(1.f, kv - 8);
-                }
+            store_codes<FULL>(avg, at, have, mc);
+            store_codes<FULL>(avg_sq, at, have, vc);
+            if (lane == 0 && (FULL || block * QBLOCK < have)) {        // an infinity or a NaN makes NaN of the whole block
+                store_global(avg_scale, 4 * block, mb == 0 ? 0.f : mb >= 0x7f800000u ? NAN : ldexpf(1.f, km - 8));
+                store_global(avg_sq_scale, 4 * block, vb == 0 ? 0.f : vb >= 0x7f800000u ? NAN : ldexpf(1.f, kv - 8));
             }
         }
-        if (have > 0) {
-            if (master) store4(t.master, at, QLORA_F32, have, wf);
-            store4(t.param, at, t.param_dtype, have, wf);
-        }
+        if (master) store4<FULL>(main, at, QLORA_F32, have, wf);
+        store4<FULL>(param, at, param_dtype, have, wf);
     }
     if (blockIdx.x == 0 && threadIdx.x == 0) {             // no other workgroup reads these
         qlora_optim_control_t *w = a.control;
@@ -348,10 +413,18 @@ __global__ __launch_bounds__(OT) void adamw_kernel(const AdamArgs a)
 {
     const u32x2_t at = a.table[blockIdx.x];
     const OptimTensor t = a.tensors[at[0]];
-    if (t.state_bits == 8)
-        step_chunk<8>(a, t, at[1]);
-    else
-        step_chunk<32>(a, t, at[1]);
+    const bool full = t.numel - (long)at[1] * CHUNK >= CHUNK;
+    if (t.state_bits == 8) {
+        if (full)
+            step_chunk<8, true>(a, t, at[1]);
+        else
+            step_chunk<8, false>(a, t, at[1]);
+    } else {
+        if (full)
+            step_chunk<32, true>(a, t, at[1]);
+        else
+            step_chunk<32, false>(a, t, at[1]);
+    }
 }
 
 inline const OptimTensor *tensors_of(const void *plan_device)
