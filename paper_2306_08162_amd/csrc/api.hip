@@ -906,7 +906,7 @@ size_t qlora_optim_plan_bytes(int count, const qlora_optim_tensor_t *tensors)
 {
     uint64_t weights, blocks, chunks;
     if (!count_weights(count, tensors, weights, blocks, chunks)) return 0;
-    return sizeof(OptimHeader) + sizeof(OptimTensor) * (size_t)count + 2 * sizeof(uint32_t) * (size_t)chunks;
+    return sizeof(OptimHeader) + sizeof(OptimChunk) * (size_t)chunks;
 }
 
 int qlora_optim_plan(int count, const qlora_optim_tensor_t *tensors, void *plan, size_t plan_bytes)
@@ -950,22 +950,23 @@ int qlora_optim_plan(int count, const qlora_optim_tensor_t *tensors, void *plan,
     char *out = (char *)plan;
     std::copy_n((const char *)&h, sizeof h, out);
     out += sizeof h;
-    char *table = out + sizeof(OptimTensor) * (size_t)count;
-    uint32_t block = 0;
+    uint32_t place = 0;
+    const auto at = [](const void *p, size_t bytes) { return p ? (char *)p + bytes : nullptr; };
     for (int i = 0; i < count; ++i) {
         const qlora_optim_tensor_t &t = tensors[i];
-        const OptimTensor o{t.param, t.grad, t.master, t.exp_avg, t.exp_avg_sq, t.avg_scale, t.avg_sq_scale, t.numel, block,
-                            t.lr_scale, t.weight_decay, (uint8_t)t.param_dtype, (uint8_t)t.grad_dtype,
-                            (uint8_t)t.state_bits, 0};
-        std::copy_n((const char *)&o, sizeof o, out);
-        out += sizeof o;
-        block += (uint32_t)((t.numel + QLORA_OPTIM_BLOCK - 1) / QLORA_OPTIM_BLOCK);    // wraps: it only feeds a hash
-        const uint32_t n = (uint32_t)((t.numel + OPTIM_CHUNK - 1) / OPTIM_CHUNK);
-        for (uint32_t c = 0; c < n; ++c) {
-            const uint32_t entry[2] = {(uint32_t)i, c};
-            std::copy_n((const char *)entry, sizeof entry, table);
-            table += sizeof entry;
+        const size_t sbytes = t.state_bits / 8;
+        for (size_t begin = 0; begin < (size_t)t.numel; begin += OPTIM_CHUNK) {
+            const size_t scales = begin / QLORA_OPTIM_BLOCK * sizeof(float);
+            const OptimChunk o{at(t.param, begin * dtype_bytes(t.param_dtype)), at(t.grad, begin * dtype_bytes(t.grad_dtype)),
+                               at(t.master, begin * 4), at(t.exp_avg, begin * sbytes), at(t.exp_avg_sq, begin * sbytes),
+                               at(t.avg_scale, scales), at(t.avg_sq_scale, scales),
+                               (uint32_t)std::min<size_t>((size_t)t.numel - begin, OPTIM_CHUNK), place + (uint32_t)begin,
+                               t.lr_scale, t.weight_decay, (uint8_t)t.param_dtype, (uint8_t)t.grad_dtype,
+                               (uint8_t)t.state_bits, 0, 0};
+            std::copy_n((const char *)&o, sizeof o, out);
+            out += sizeof o;
         }
+        place += (uint32_t)((t.numel + QLORA_OPTIM_BLOCK - 1) / QLORA_OPTIM_BLOCK) * QLORA_OPTIM_BLOCK;    // wraps
     }
     return QLORA_OK;
 }

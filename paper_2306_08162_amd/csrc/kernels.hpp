@@ -197,11 +197,10 @@ void launch_token_logprobs_bwd(const void *logits, long stride, const int32_t *t
                                const float *d_logprob, const float *d_entropy, void *dlogits, long d_stride, int M, int V,
                                int dt, hipStream_t s);
 
-// optim.hip -- AdamW over many tensors and the norm of their gradients.  A plan is a header, one record a tensor, and for
-// each chunk of OPTIM_CHUNK weights the tensor it belongs to and its number in there; the kernels read the copy in device
-// memory, the launchers the header alone.
-constexpr int OPTIM_CHUNK = 4096;
-constexpr unsigned OPTIM_PARTS = 1024;         // workgroups of the sum of squares, one partial sum each
+// optim.hip -- AdamW over many tensors and the norm of their gradients.  A plan is a header and a record for each chunk of
+// up to OPTIM_CHUNK weights of a tensor; the kernels read the copy in device memory, the launchers the header alone.
+constexpr int OPTIM_CHUNK = 2048;
+constexpr unsigned OPTIM_PARTS = 256;          // workgroups of the sum of squares, one partial sum each
 constexpr uint64_t OPTIM_MAGIC = 0x3170a4d4f5157ull;
 struct OptimHeader {
     uint64_t magic, bytes, weights;
@@ -210,18 +209,19 @@ struct OptimHeader {
     uint32_t reserved[7];
 };
 static_assert(sizeof(OptimHeader) == 64, "plan layout");
-struct OptimTensor {
+struct OptimChunk {                            // one workgroup's work: one record, no second look-up behind it
     void *param;
     const void *grad;
-    float *master;                             // NULL: param itself is updated
+    void *master;                              // NULL: param itself is updated
     void *exp_avg, *exp_avg_sq;
-    float *avg_scale, *avg_sq_scale;           // 8-bit states
-    int64_t numel;
-    uint32_t first_block;                      // blocks of weights of the tensors before it
+    void *avg_scale, *avg_sq_scale;            // 8-bit states
+    uint32_t weights;                          // of the chunk
+    uint32_t place;                            // of its first weight in the plan, tensors beginning at whole blocks (it feeds a hash)
     float lr_scale, weight_decay;
     uint8_t param_dtype, grad_dtype, state_bits, reserved;
+    uint32_t unused;
 };
-static_assert(sizeof(OptimTensor) == 80, "plan layout");
+static_assert(sizeof(OptimChunk) == 80, "plan layout");
 // parts: OPTIM_PARTS doubles
 void launch_grad_norm(const OptimHeader &h, const void *plan_device, float grad_scale, float *norm, double *parts,
                       hipStream_t s);

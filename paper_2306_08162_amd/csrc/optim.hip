@@ -4,8 +4,8 @@
 //   w = w (1 - lr wd) - lr / (1 - b1^t) * m / (sqrt(v) / sqrt(1 - b2^t) + eps)
 //
 // The step is bound by HBM: with fp32 gradients and 16-bit weights 24 bytes a weight (fp32 states), 12 with states of
-// 8 bits.  A plan in device memory lists the tensors and, for each chunk of 4096 weights, whose it is: the grid is the
-// chunks of all tensors, so hundreds of small matrices fill the chip like one large one.
+// 8 bits.  A plan in device memory has a record for each chunk of up to 2048 weights of a tensor, one workgroup's work: hundreds
+// of small matrices fill the chip like one large one.
 //
 // 8-bit states.  256 consecutive weights share a scale, the power of two that brings the largest magnitude into
 // (224, 448]; the codes are e4m3, which keeps four significant bits over 17 powers of two, and a power of two for a scale
@@ -128,9 +128,6 @@ __device__ __forceinline__ void store_codes(void *p, uint32_t i, uint32_t have, 
         for (uint32_t e = 0; e < 3; ++e)
             if (i + e < have) store_global(p, i + e, (uint8_t)(r >> (8 * e)));
 }
-__device__ __forceinline__ uint32_t size_of(int dtype) { return dtype == QLORA_F32 ? 4 : 2; }
-__device__ __forceinline__ void *advance(const void *p, uint64_t bytes) { return (char *)p + bytes; }
-
 __device__ __forceinline__ void decode4(uint32_t codes, float scale, float *f)
 {
     const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, true);
@@ -216,41 +213,38 @@ __device__ __forceinline__ void prepare_step(qlora_optim_control_t *c, double be
 __global__ void adamw_prepare_kernel(qlora_optim_control_t *c, double beta1, double beta2) { prepare_step(c, beta1, beta2); }
 
 // parts[workgroup] = sum of the squares of its chunks' gradients, in 64 bits: no square leaves the range, and the sum of
-// hundreds of millions of them keeps more than the 24 bits of the result
-__global__ __launch_bounds__(OT) void grad_square_kernel(const OptimTensor *__restrict__ tensors,
-                                                         const u32x2_t *__restrict__ table, uint32_t chunks,
+// hundreds of millions of them keeps more than the 24 bits of the result.  Each quarter of a workgroup has chunks of its own.
+// One workgroup a compute unit and no more: every workgroup of the step reads all partial sums (with 1024 of them that
+// was as much traffic as the gradients of 160 million weights).
+constexpr int ST = 4 * OT;
+__global__ __launch_bounds__(ST) void grad_square_kernel(const OptimChunk *__restrict__ table, uint32_t chunks,
                                                          double *parts, qlora_optim_control_t *control, double beta1,
                                                          double beta2)
 {
     if (control && blockIdx.x == 0 && threadIdx.x == 0) prepare_step(control, beta1, beta2);
+    const uint32_t quarter = __builtin_amdgcn_readfirstlane(threadIdx.x / OT), tid = threadIdx.x & (OT - 1);
     // whose chunk is next is found out while this one's gradients are on their way
     struct Place {
         const void *grad;
         uint32_t have;
         int dtype;
     };
-    const auto place = [&](uint32_t c) {
-        const u32x2_t at = table[c];
-        const OptimTensor *t = tensors + at[0];
-        const long left = t->numel - (long)at[1] * CHUNK;
-        return Place{advance(t->grad, (uint64_t)at[1] * CHUNK * size_of(t->grad_dtype)),
-                     (uint32_t)(left < CHUNK ? left : CHUNK), t->grad_dtype};
-    };
+    const auto place = [&](uint32_t c) { return Place{table[c].grad, table[c].weights, table[c].grad_dtype}; };
     double s = 0.0;
-    uint32_t c = blockIdx.x;
-    Place next = place(c);
+    uint32_t c = blockIdx.x + quarter * gridDim.x;
+    Place next{};
+    if (c < chunks) next = place(c);
     while (c < chunks) {
         const Place now = next;
         u32x4_t g[PASSES];
         if (now.have == CHUNK) {
 #pragma unroll
-            for (int i = 0; i < PASSES; ++i) g[i] = load4<true>(now.grad, (i * OT + threadIdx.x) * 4, now.dtype, CHUNK);
+            for (int i = 0; i < PASSES; ++i) g[i] = load4<true>(now.grad, (i * OT + tid) * 4, now.dtype, CHUNK);
         } else {
 #pragma unroll
-            for (int i = 0; i < PASSES; ++i)
-                g[i] = load4<false>(now.grad, (i * OT + threadIdx.x) * 4, now.dtype, now.have);
+            for (int i = 0; i < PASSES; ++i) g[i] = load4<false>(now.grad, (i * OT + tid) * 4, now.dtype, now.have);
         }
-        c += gridDim.x;
+        c += 4 * gridDim.x;
         if (c < chunks) next = place(c);
 #pragma unroll
         for (int i = 0; i < PASSES; ++i) {
@@ -260,12 +254,17 @@ __global__ __launch_bounds__(OT) void grad_square_kernel(const OptimTensor *__re
             for (int e = 0; e < 4; ++e) s = fma((double)f[e], (double)f[e], s);
         }
     }
-    __shared__ double red[OT / 64];
+    __shared__ double red[ST / 64];
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off, WAVE);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
     __syncthreads();
-    if (threadIdx.x == 0) parts[blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
+    if (threadIdx.x < 16) {
+        s = red[threadIdx.x];
+#pragma unroll
+        for (int off = 8; off > 0; off >>= 1) s += __shfl_xor(s, off, 16);
+        if (threadIdx.x == 0) parts[blockIdx.x] = s;
+    }
 }
 
 __global__ __launch_bounds__(OT) void grad_norm_kernel(const double *__restrict__ parts, int count, float grad_scale,
@@ -276,8 +275,7 @@ __global__ __launch_bounds__(OT) void grad_norm_kernel(const double *__restrict_
 }
 
 struct AdamArgs {
-    const OptimTensor *tensors;
-    const u32x2_t *table;
+    const OptimChunk *table;
     qlora_optim_control_t *control;
     const double *parts;
     int count;                       // partial sums; 0: gradients are neither checked nor clipped
@@ -304,42 +302,36 @@ __device__ __forceinline__ void adam4(const AdamArgs &a, const AdamCoef &c, cons
 }
 
 template <int BITS, bool FULL>
-__device__ __forceinline__ void step_chunk(const AdamArgs &a, const OptimTensor &t, uint32_t chunk)
+__device__ __forceinline__ void step_chunk(const AdamArgs &a, const OptimChunk &t)
 {
-    const uint64_t begin = (uint64_t)chunk * CHUNK;
-    const long left = t.numel - (long)begin;
-    const uint32_t have = FULL ? CHUNK : (uint32_t)(left < CHUNK ? left : CHUNK);
+    const uint32_t have = FULL ? CHUNK : t.weights;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const bool master = t.master != nullptr;
     const int wide = master ? (int)QLORA_F32 : t.param_dtype, grad_dtype = t.grad_dtype, param_dtype = t.param_dtype;
-    constexpr int SBYTES = BITS / 8;
-    const void *grad = advance(t.grad, begin * size_of(grad_dtype));
-    void *param = advance(t.param, begin * size_of(param_dtype)), *main = master ? advance(t.master, begin * 4) : param;
-    void *avg = advance(t.exp_avg, begin * SBYTES), *avg_sq = advance(t.exp_avg_sq, begin * SBYTES);
-    void *avg_scale = advance(t.avg_scale, begin / QBLOCK * 4), *avg_sq_scale = advance(t.avg_sq_scale, begin / QBLOCK * 4);
+    void *const main = master ? t.master : t.param;
     u32x4_t g[PASSES], w[PASSES], m[PASSES], v[PASSES];
     float ms[PASSES], vs[PASSES];
 #pragma unroll
     for (int i = 0; i < PASSES; ++i) {
         const uint32_t at = (i * OT + threadIdx.x) * 4;
-        g[i] = load4<FULL>(grad, at, grad_dtype, have);
+        g[i] = load4<FULL>(t.grad, at, grad_dtype, have);
         w[i] = load4<FULL>(main, at, wide, have);
         if constexpr (BITS == 32) {
-            m[i] = load4<FULL>(avg, at, QLORA_F32, have);
-            v[i] = load4<FULL>(avg_sq, at, QLORA_F32, have);
+            m[i] = load4<FULL>(t.exp_avg, at, QLORA_F32, have);
+            v[i] = load4<FULL>(t.exp_avg_sq, at, QLORA_F32, have);
         } else {
             const uint32_t block = i * (OT / 64) + wave;               // the wave's
             const bool some = FULL || block * QBLOCK < have;
-            m[i][0] = load_codes<FULL>(avg, at, have);
-            v[i][0] = load_codes<FULL>(avg_sq, at, have);
-            ms[i] = some ? load_global<float>(avg_scale, 4 * block) : 0.f;
-            vs[i] = some ? load_global<float>(avg_sq_scale, 4 * block) : 0.f;
+            m[i][0] = load_codes<FULL>(t.exp_avg, at, have);
+            v[i][0] = load_codes<FULL>(t.exp_avg_sq, at, have);
+            ms[i] = some ? load_global<float>(t.avg_scale, 4 * block) : 0.f;
+            vs[i] = some ? load_global<float>(t.avg_sq_scale, 4 * block) : 0.f;
         }
     }
     const qlora_optim_control_t *ctl = a.control;
     float gscale = ctl->grad_scale;
     const float lr = ctl->lr, rate = ctl->rate * t.lr_scale, root = ctl->root;
-    const uint32_t key = ctl->key + (t.first_block + (uint32_t)(begin / QBLOCK)) * QBLOCK + lane * 4;
+    const uint32_t key = ctl->key + t.place + lane * 4;
     if (a.count > 0) {
         const double norm = sqrt(sum_parts(a.parts, a.count)) * fabs((double)gscale);
         const bool finite = (float)norm < INFINITY;
@@ -369,8 +361,8 @@ __device__ __forceinline__ void step_chunk(const AdamArgs &a, const OptimTensor 
         }
         adam4(a, c, gf, mf, vf, uf, wf);
         if constexpr (BITS == 32) {
-            store4<FULL>(avg, at, QLORA_F32, have, mf);
-            store4<FULL>(avg_sq, at, QLORA_F32, have, vf);
+            store4<FULL>(t.exp_avg, at, QLORA_F32, have, mf);
+            store4<FULL>(t.exp_avg_sq, at, QLORA_F32, have, vf);
         } else {
             uint32_t mb = 0, vb = 0;
 #pragma unroll
@@ -391,15 +383,15 @@ __device__ __forceinline__ void step_chunk(const AdamArgs &a, const OptimTensor 
                 const uint32_t q = encode_root(uf[e], kv, r & 0xfffffu);
                 vc |= (q == 0 && vf[e] > 0.f ? 1u : q) << (8 * e);
             }
-            store_codes<FULL>(avg, at, have, mc);
-            store_codes<FULL>(avg_sq, at, have, vc);
+            store_codes<FULL>(t.exp_avg, at, have, mc);
+            store_codes<FULL>(t.exp_avg_sq, at, have, vc);
             if (lane == 0 && (FULL || block * QBLOCK < have)) {        // an infinity or a NaN makes NaN of the whole block
-                store_global(avg_scale, 4 * block, mb == 0 ? 0.f : mb >= 0x7f800000u ? NAN : ldexpf(1.f, km - 8));
-                store_global(avg_sq_scale, 4 * block, vb == 0 ? 0.f : vb >= 0x7f800000u ? NAN : ldexpf(1.f, kv - 8));
+                store_global(t.avg_scale, 4 * block, mb == 0 ? 0.f : mb >= 0x7f800000u ? NAN : ldexpf(1.f, km - 8));
+                store_global(t.avg_sq_scale, 4 * block, vb == 0 ? 0.f : vb >= 0x7f800000u ? NAN : ldexpf(1.f, kv - 8));
             }
         }
         if (master) store4<FULL>(main, at, QLORA_F32, have, wf);
-        store4<FULL>(param, at, param_dtype, have, wf);
+        store4<FULL>(t.param, at, param_dtype, have, wf);
     }
     if (blockIdx.x == 0 && threadIdx.x == 0) {             // no other workgroup reads these
         qlora_optim_control_t *w = a.control;
@@ -411,40 +403,35 @@ __device__ __forceinline__ void step_chunk(const AdamArgs &a, const OptimTensor 
 
 __global__ __launch_bounds__(OT) void adamw_kernel(const AdamArgs a)
 {
-    const u32x2_t at = a.table[blockIdx.x];
-    const OptimTensor t = a.tensors[at[0]];
-    const bool full = t.numel - (long)at[1] * CHUNK >= CHUNK;
+    const OptimChunk t = a.table[blockIdx.x];
+    const bool full = t.weights == CHUNK;
     if (t.state_bits == 8) {
         if (full)
-            step_chunk<8, true>(a, t, at[1]);
+            step_chunk<8, true>(a, t);
         else
-            step_chunk<8, false>(a, t, at[1]);
+            step_chunk<8, false>(a, t);
     } else {
         if (full)
-            step_chunk<32, true>(a, t, at[1]);
+            step_chunk<32, true>(a, t);
         else
-            step_chunk<32, false>(a, t, at[1]);
+            step_chunk<32, false>(a, t);
     }
 }
 
-inline const OptimTensor *tensors_of(const void *plan_device)
+inline const OptimChunk *table_of(const void *plan_device)
 {
-    return (const OptimTensor *)((const char *)plan_device + sizeof(OptimHeader));
+    return (const OptimChunk *)((const char *)plan_device + sizeof(OptimHeader));
 }
-inline const u32x2_t *table_of(const OptimHeader &h, const void *plan_device)
-{
-    return (const u32x2_t *)(tensors_of(plan_device) + h.count);
-}
+inline unsigned square_grid(const OptimHeader &h) { return h.chunks < OPTIM_PARTS ? h.chunks : OPTIM_PARTS; }
 
 }  // namespace
 
 void launch_grad_norm(const OptimHeader &h, const void *plan_device, float grad_scale, float *norm, double *parts,
                       hipStream_t s)
 {
-    const unsigned grid = h.chunks < OPTIM_PARTS ? h.chunks : OPTIM_PARTS;
-    if (grid > 0)
-        QLORA_LAUNCH(grad_square_kernel, dim3(grid), dim3(OT), 0, s, tensors_of(plan_device), table_of(h, plan_device),
-                     h.chunks, parts, (qlora_optim_control_t *)nullptr, 0.0, 0.0);
+    const unsigned grid = square_grid(h);
+    QLORA_LAUNCH(grad_square_kernel, dim3(grid), dim3(ST), 0, s, table_of(plan_device), h.chunks, parts,
+                 (qlora_optim_control_t *)nullptr, 0.0, 0.0);
     QLORA_LAUNCH(grad_norm_kernel, dim3(1), dim3(OT), 0, s, parts, (int)grid, grad_scale, norm);
 }
 
@@ -452,14 +439,13 @@ void launch_adamw(const OptimHeader &h, const void *plan_device, void *control, 
                   double max_norm, double *parts, hipStream_t s)
 {
     qlora_optim_control_t *c = (qlora_optim_control_t *)control;
-    const unsigned grid = h.chunks < OPTIM_PARTS ? h.chunks : OPTIM_PARTS;
+    const unsigned grid = square_grid(h);
     const bool guarded = max_norm > 0.0;
     if (guarded)
-        QLORA_LAUNCH(grad_square_kernel, dim3(grid), dim3(OT), 0, s, tensors_of(plan_device), table_of(h, plan_device),
-                     h.chunks, parts, c, beta1, beta2);
+        QLORA_LAUNCH(grad_square_kernel, dim3(grid), dim3(ST), 0, s, table_of(plan_device), h.chunks, parts, c, beta1, beta2);
     else
         QLORA_LAUNCH(adamw_prepare_kernel, dim3(1), dim3(1), 0, s, c, beta1, beta2);
-    const AdamArgs a{tensors_of(plan_device), table_of(h, plan_device), c, parts, guarded ? (int)grid : 0, beta1, beta2,
+    const AdamArgs a{table_of(plan_device), c, parts, guarded ? (int)grid : 0, beta1, beta2,
                      max_norm, (float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)eps};
     QLORA_LAUNCH(adamw_kernel, dim3(h.chunks), dim3(OT), 0, s, a);
 }

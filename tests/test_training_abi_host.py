@@ -87,17 +87,17 @@ def test_plan_layout():
     tensors = [_tensor(at=0x10000000 * (i + 1), n=n, lr_scale=2.0 + i) for i, n in enumerate((1, 4096, 0, 4097, 300))]
     plan, st = ql.qlora_optim_plan(tensors, check=False)
     assert st == 0
-    assert ql.qlora_optim_plan_bytes(tensors) == 64 + 5 * 80 + 8 * 5 == len(plan.raw)
+    assert ql.qlora_optim_plan_bytes(tensors) == 64 + 80 * 7 == len(plan.raw)
     magic, nbytes, weights, count, chunks, steppable = struct.unpack_from("<QQQIII", plan.raw)
-    assert (nbytes, weights, count, chunks, steppable) == (len(plan.raw), 1 + 4096 + 4097 + 300, 5, 5, 1)
-    blocks = []
-    for i, t in enumerate(tensors):
-        rec = struct.unpack_from("<7QqIffBBBB", plan.raw, 64 + 80 * i)
-        assert rec[7] == t.numel and rec[9] == 2.0 + i and rec[11:14] == (0, 2, 8)
-        blocks.append(rec[8])
-    assert blocks == [0, 1, 17, 17, 34]
-    table = [struct.unpack_from("<II", plan.raw, 64 + 5 * 80 + 8 * c) for c in range(5)]
-    assert table == [(0, 0), (1, 0), (3, 0), (3, 1), (4, 0)]
+    assert (nbytes, weights, count, chunks, steppable) == (len(plan.raw), 1 + 4096 + 4097 + 300, 5, 7, 1)
+    got = [struct.unpack_from("<7QIIffBBBB", plan.raw, 64 + 80 * c) for c in range(7)]
+    # (tensor, first weight, weights, place in the plan): tensors begin at whole blocks of 256
+    for rec, (i, begin, n, place) in zip(got, [(0, 0, 1, 0), (1, 0, 2048, 256), (1, 2048, 2048, 2304), (3, 0, 2048, 4352),
+                                               (3, 2048, 2048, 6400), (3, 4096, 1, 8448), (4, 0, 300, 8704)]):
+        t = tensors[i]
+        assert rec[7:10] == (n, place, 2.0 + i) and rec[11:14] == (0, 2, 8)
+        assert rec[:7] == (t.param + 2 * begin, t.grad + 4 * begin, t.master + 4 * begin, t.exp_avg + begin,
+                           t.exp_avg_sq + begin, t.avg_scale + begin // 64, t.avg_sq_scale + begin // 64)
 
 
 def test_plan_bytes_of_nothing():
