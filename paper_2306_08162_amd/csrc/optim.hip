@@ -175,31 +175,38 @@ __device__ __forceinline__ int root_scale_of(uint32_t bits)
     return ((((b + 0x3bffff) >> 23) - 127) >> 1);
 }
 
-// |x| <= 1.75 * 2^k, 0 <= r < 2^20: the e4m3 code of x / 2^(k - 8), rounded up where r exceeds the distance.  Multiplied by 2^-112
-// (k taken off first) the code's exponent and mantissa are the top bits of the float, below the smallest normal code too.
+// |x| <= 1.75 * 2^k, 0 <= r < 2^20: the e4m3 code of x / 2^(k - 8), rounded up where r exceeds the distance, in the top byte.
+// Multiplied by 2^-112 (k taken off first) the code's exponent and mantissa are bits 26..20 of the float, below the smallest
+// normal code too; what is under them does not matter.
 __device__ __forceinline__ uint32_t encode(float x, int k, uint32_t r)
 {
     const uint32_t y = __float_as_uint(ldexpf(fabsf(x), -112 - k));
-    return ((y + r) >> 20) | (__float_as_uint(x) >> 24 & 0x80u);
+    return (((y + r) << 4) & 0x7fffffffu) | (__float_as_uint(x) & 0x80000000u);
 }
-// the same for x >= 0 that is a hardware square root: it may lie one unit above 1.75 * 2^k
-__device__ __forceinline__ uint32_t encode_root(float x, int k, uint32_t r)
+// The same for u = sqrt(v), which the hardware may leave one unit above 1.75 * 2^k; at least code 1 where v > 0.
+__device__ __forceinline__ uint32_t encode_root(float u, float v, int k, uint32_t r)
 {
-    const uint32_t y = __float_as_uint(fminf(ldexpf(x, -112 - k), 1.75f * 0x1p-112f));
-    return (y + r) >> 20;
+    const uint32_t y = __float_as_uint(fminf(ldexpf(u, -112 - k), 1.75f * 0x1p-112f)) + r, least = v > 0.f ? 1u << 20 : 0u;
+    return (y > least ? y : least) << 4;
+}
+// the top bytes of four words as one word
+__device__ __forceinline__ uint32_t top_bytes(const uint32_t *t)
+{
+    return __builtin_amdgcn_perm(t[1], t[0], 0x0c0c0703u) | __builtin_amdgcn_perm(t[3], t[2], 0x07030c0cu);
 }
 
-// the sum of the partial sums, the same in every thread of every workgroup
+// the sum of the partial sums in every lane of a wave, the same in every wave
 __device__ __forceinline__ double sum_parts(const double *__restrict__ parts, int count)
 {
-    __shared__ double red[OT / 64];
     double v = 0.0;
-    for (int i = threadIdx.x; i < count; i += OT) v += parts[i];
+#pragma unroll
+    for (int i = 0; i < (int)OPTIM_PARTS; i += WAVE) {
+        const int at = i + (threadIdx.x & 63);
+        v += at < count ? parts[at] : 0.0;
+    }
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, WAVE);
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    return (red[0] + red[1]) + (red[2] + red[3]);
+    return v;
 }
 
 // what the coming step needs of the control block; nothing but this and the step's last lines writes there
@@ -267,7 +274,7 @@ __global__ __launch_bounds__(ST) void grad_square_kernel(const OptimChunk *__res
     }
 }
 
-__global__ __launch_bounds__(OT) void grad_norm_kernel(const double *__restrict__ parts, int count, float grad_scale,
+__global__ __launch_bounds__(WAVE) void grad_norm_kernel(const double *__restrict__ parts, int count, float grad_scale,
                                                        float *norm)
 {
     const double s = sum_parts(parts, count);
@@ -287,6 +294,7 @@ struct AdamCoef {
     float gscale, decay, rate, root;
 };
 
+// m = its old value times b1 on the way in
 __device__ __forceinline__ void adam4(const AdamArgs &a, const AdamCoef &c, const float *g, float *m, float *v, float *u,
                                       float *w)
 {
@@ -294,7 +302,7 @@ __device__ __forceinline__ void adam4(const AdamArgs &a, const AdamCoef &c, cons
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         const float x = g[e] * c.gscale;
-        m[e] = m[e] * a.b1 + x * a.c1;
+        m[e] = m[e] + x * a.c1;
         v[e] = v[e] * a.b2 + (x * x) * a.c2;
         u[e] = __builtin_amdgcn_sqrtf(v[e]);
         w[e] = w[e] * c.decay - c.rate * (m[e] * __builtin_amdgcn_rcpf(u[e] * c.root + a.eps));
@@ -333,15 +341,19 @@ __device__ __forceinline__ void step_chunk(const AdamArgs &a, const OptimChunk &
     const float lr = ctl->lr, rate = ctl->rate * t.lr_scale, root = ctl->root;
     const uint32_t key = ctl->key + t.place + lane * 4;
     if (a.count > 0) {
-        const double norm = sqrt(sum_parts(a.parts, a.count)) * fabs((double)gscale);
-        const bool finite = (float)norm < INFINITY;
-        if (blockIdx.x == 0 && threadIdx.x == 0) {
-            a.control->grad_norm = (float)norm;
-            if (!finite) a.control->skipped += 1;
+        __shared__ float clipped;                                      // NaN: the step is not taken
+        if (wave == 0) {
+            const double norm = sqrt(sum_parts(a.parts, a.count)) * fabs((double)gscale), clip = a.max_norm / norm;
+            const bool finite = (float)norm < INFINITY;
+            if (lane == 0) clipped = finite ? gscale * (float)(clip < 1.0 ? clip : 1.0) : NAN;     // (norm 0: nothing to clip)
+            if (blockIdx.x == 0 && lane == 0) {
+                a.control->grad_norm = (float)norm;
+                if (!finite) a.control->skipped += 1;
+            }
         }
-        if (!finite) return;                                           // the step is not taken
-        const double clip = a.max_norm / norm;
-        gscale *= (float)(clip < 1.0 ? clip : 1.0);                    // (norm 0: no gradient to clip)
+        __syncthreads();
+        gscale = clipped;
+        if (gscale != gscale) return;
     }
     const AdamCoef c{gscale, 1.f - lr * t.lr_scale * t.weight_decay, rate, root};
 #pragma unroll
@@ -353,8 +365,10 @@ __device__ __forceinline__ void step_chunk(const AdamArgs &a, const OptimChunk &
         if constexpr (BITS == 32) {
             widen4(m[i], QLORA_F32, mf);
             widen4(v[i], QLORA_F32, vf);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) mf[e] *= a.b1;
         } else {
-            decode4(m[i][0], ms[i], mf);
+            decode4(m[i][0], ms[i] * a.b1, mf);                        // a power of two times b1: one rounding in all, as in 32 bits
             decode4(v[i][0], vs[i], vf);
 #pragma unroll
             for (int e = 0; e < 4; ++e) vf[e] *= vf[e];
@@ -364,30 +378,29 @@ __device__ __forceinline__ void step_chunk(const AdamArgs &a, const OptimChunk &
             store4<FULL>(t.exp_avg, at, QLORA_F32, have, mf);
             store4<FULL>(t.exp_avg_sq, at, QLORA_F32, have, vf);
         } else {
-            uint32_t mb = 0, vb = 0;
+            const uint32_t mb = wave_max_bits(__float_as_uint(
+                fmaxf(fmaxf(fabsf(mf[0]), fabsf(mf[1])), fmaxf(fabsf(mf[2]), fabsf(mf[3])))));
+            uint32_t vb = 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t p = __float_as_uint(fabsf(mf[e])), q = __float_as_uint(vf[e]);
-                mb = mb > p ? mb : p;
-                vb = vb > q ? vb : q;
-            }
-            mb = wave_max_bits(mb);
+            for (int e = 0; e < 4; ++e) vb = vb > __float_as_uint(vf[e]) ? vb : __float_as_uint(vf[e]);
             vb = wave_max_bits(vb);
             const int km = scale_of(mb), kv = root_scale_of(vb);
             const uint32_t block = i * (OT / 64) + wave;
-            uint32_t mc = 0, vc = 0;
+            uint32_t mc[4], vc[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const uint32_t r = mix(key + block * QBLOCK + e);
-                mc |= encode(mf[e], km, r >> 12) << (8 * e);
-                const uint32_t q = encode_root(uf[e], kv, r & 0xfffffu);
-                vc |= (q == 0 && vf[e] > 0.f ? 1u : q) << (8 * e);
+                mc[e] = encode(mf[e], km, r >> 12);
+                vc[e] = encode_root(uf[e], vf[e], kv, r & 0xfffffu);
             }
-            store_codes<FULL>(t.exp_avg, at, have, mc);
-            store_codes<FULL>(t.exp_avg_sq, at, have, vc);
-            if (lane == 0 && (FULL || block * QBLOCK < have)) {        // an infinity or a NaN makes NaN of the whole block
-                store_global(t.avg_scale, 4 * block, mb == 0 ? 0.f : mb >= 0x7f800000u ? NAN : ldexpf(1.f, km - 8));
-                store_global(t.avg_sq_scale, 4 * block, vb == 0 ? 0.f : vb >= 0x7f800000u ? NAN : ldexpf(1.f, kv - 8));
+            store_codes<FULL>(t.exp_avg, at, have, top_bytes(mc));
+            store_codes<FULL>(t.exp_avg_sq, at, have, top_bytes(vc));
+            // A gradient that is not finite leaves v so too, and makes NaN of the whole block (m of a NaN alone shows nothing: the
+            // maximum passes over it).
+            const bool bad = vb >= 0x7f800000u;
+            if (lane == 0 && (FULL || block * QBLOCK < have)) {
+                store_global(t.avg_scale, 4 * block, bad ? NAN : mb == 0 ? 0.f : ldexpf(1.f, km - 8));
+                store_global(t.avg_sq_scale, 4 * block, bad ? NAN : vb == 0 ? 0.f : ldexpf(1.f, kv - 8));
             }
         }
         if (master) store4<FULL>(main, at, QLORA_F32, have, wf);
@@ -432,7 +445,7 @@ void launch_grad_norm(const OptimHeader &h, const void *plan_device, float grad_
     const unsigned grid = square_grid(h);
     QLORA_LAUNCH(grad_square_kernel, dim3(grid), dim3(ST), 0, s, table_of(plan_device), h.chunks, parts,
                  (qlora_optim_control_t *)nullptr, 0.0, 0.0);
-    QLORA_LAUNCH(grad_norm_kernel, dim3(1), dim3(OT), 0, s, parts, (int)grid, grad_scale, norm);
+    QLORA_LAUNCH(grad_norm_kernel, dim3(1), dim3(WAVE), 0, s, parts, (int)grid, grad_scale, norm);
 }
 
 void launch_adamw(const OptimHeader &h, const void *plan_device, void *control, double beta1, double beta2, double eps,
