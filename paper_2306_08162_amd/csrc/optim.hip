@@ -195,18 +195,50 @@ __device__ __forceinline__ uint32_t top_bytes(const uint32_t *t)
     return __builtin_amdgcn_perm(t[1], t[0], 0x0c0c0703u) | __builtin_amdgcn_perm(t[3], t[2], 0x07030c0cu);
 }
 
-// the sum of the partial sums in every lane of a wave, the same in every wave
-__device__ __forceinline__ double sum_parts(const double *__restrict__ parts, int count)
+// the sum over a wave, in every lane
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double add_dpp(double v)
 {
-    double v = 0.0;
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, ROWS, 0xf, false),
+                   hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), CTRL, ROWS, 0xf, false);
+    return v + __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double wave_sum_f64(double v)
+{
+    v = add_dpp<0x111, 0xf>(v);
+    v = add_dpp<0x112, 0xf>(v);
+    v = add_dpp<0x114, 0xf>(v);
+    v = add_dpp<0x118, 0xf>(v);
+    v = add_dpp<0x142, 0xa>(v);
+    v = add_dpp<0x143, 0xc>(v);
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)b, 63),
+                   hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), 63);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+
+// A lane's share of the partial sums, and the sum of all of them in every lane of a wave.  A workgroup's first wave asks for
+// its share before anything else, and adds while its chunk is on the way.
+struct Parts {
+    double v[OPTIM_PARTS / WAVE];
+};
+__device__ __forceinline__ Parts load_parts(const double *__restrict__ parts, int count)
+{
+    Parts p;
 #pragma unroll
-    for (int i = 0; i < (int)OPTIM_PARTS; i += WAVE) {
-        const int at = i + (threadIdx.x & 63);
-        v += at < count ? parts[at] : 0.0;
+    for (int i = 0; i < (int)(OPTIM_PARTS / WAVE); ++i) {
+        const int at = i * WAVE + (threadIdx.x & 63);
+        p.v[i] = at < count ? parts[at] : 0.0;
     }
+    return p;
+}
+__device__ __forceinline__ double sum_parts(const Parts &p)
+{
+    double v = p.v[0];
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, WAVE);
-    return v;
+    for (int i = 1; i < (int)(OPTIM_PARTS / WAVE); ++i) v += p.v[i];
+    return wave_sum_f64(v);
 }
 
 // what the coming step needs of the control block; nothing but this and the step's last lines writes there
@@ -262,14 +294,11 @@ __global__ __launch_bounds__(ST) void grad_square_kernel(const OptimChunk *__res
         }
     }
     __shared__ double red[ST / 64];
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off, WAVE);
+    s = wave_sum_f64(s);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
     __syncthreads();
-    if (threadIdx.x < 16) {
-        s = red[threadIdx.x];
-#pragma unroll
-        for (int off = 8; off > 0; off >>= 1) s += __shfl_xor(s, off, 16);
+    if (threadIdx.x < 64) {
+        s = wave_sum_f64(threadIdx.x < ST / 64 ? red[threadIdx.x] : 0.0);
         if (threadIdx.x == 0) parts[blockIdx.x] = s;
     }
 }
@@ -277,7 +306,7 @@ __global__ __launch_bounds__(ST) void grad_square_kernel(const OptimChunk *__res
 __global__ __launch_bounds__(WAVE) void grad_norm_kernel(const double *__restrict__ parts, int count, float grad_scale,
                                                        float *norm)
 {
-    const double s = sum_parts(parts, count);
+    const double s = sum_parts(load_parts(parts, count));
     if (threadIdx.x == 0) norm[0] = (float)(sqrt(s) * fabs((double)grad_scale));
 }
 
@@ -310,7 +339,7 @@ __device__ __forceinline__ void adam4(const AdamArgs &a, const AdamCoef &c, cons
 }
 
 template <int BITS, bool FULL>
-__device__ __forceinline__ void step_chunk(const AdamArgs &a, const OptimChunk &t)
+__device__ __forceinline__ void step_chunk(const AdamArgs &a, const OptimChunk &t, const Parts &parts)
 {
     const uint32_t have = FULL ? CHUNK : t.weights;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -343,7 +372,7 @@ __device__ __forceinline__ void step_chunk(const AdamArgs &a, const OptimChunk &
     if (a.count > 0) {
         __shared__ float clipped;                                      // NaN: the step is not taken
         if (wave == 0) {
-            const double norm = sqrt(sum_parts(a.parts, a.count)) * fabs((double)gscale), clip = a.max_norm / norm;
+            const double norm = sqrt(sum_parts(parts)) * fabs((double)gscale), clip = a.max_norm / norm;
             const bool finite = (float)norm < INFINITY;
             if (lane == 0) clipped = finite ? gscale * (float)(clip < 1.0 ? clip : 1.0) : NAN;     // (norm 0: nothing to clip)
             if (blockIdx.x == 0 && lane == 0) {
@@ -416,18 +445,20 @@ __device__ __forceinline__ void step_chunk(const AdamArgs &a, const OptimChunk &
 
 __global__ __launch_bounds__(OT) void adamw_kernel(const AdamArgs a)
 {
+    Parts parts{};
+    if (a.count > 0 && threadIdx.x < WAVE) parts = load_parts(a.parts, a.count);
     const OptimChunk t = a.table[blockIdx.x];
     const bool full = t.weights == CHUNK;
     if (t.state_bits == 8) {
         if (full)
-            step_chunk<8, true>(a, t);
+            step_chunk<8, true>(a, t, parts);
         else
-            step_chunk<8, false>(a, t);
+            step_chunk<8, false>(a, t, parts);
     } else {
         if (full)
-            step_chunk<32, true>(a, t);
+            step_chunk<32, true>(a, t, parts);
         else
-            step_chunk<32, false>(a, t);
+            step_chunk<32, false>(a, t, parts);
     }
 }
 

@@ -349,6 +349,9 @@ class AdapterOptimizer:
         control = ql.qlora_optim_control_init(lr, grad_scale, seed, step, *self.betas)
         self.control = self._upload(control)
         self.workspace = torch.empty(ql.qlora_optim_workspace_bytes(), dtype=torch.uint8, device=self.device)
+        # taken once: a step's host time is that of its two launches
+        self._plan_ptr, self._control_ptr = self.plan_device.data_ptr(), self.control.data_ptr()
+        self._workspace_ptr, self._workspace_bytes = self.workspace.data_ptr(), self.workspace.numel()
         words = self.control.view(torch.float32)
         self.lr, self.last_grad_norm = words[0:1], words[5:6]               # device floats: write lr, read the norm
         self.device_grad_scale = words[1:2]
@@ -403,11 +406,11 @@ class AdapterOptimizer:
 
     def step(self, stream=None) -> None:
         self._here()
-        ql.qlora_adamw_step(self.plan, self.plan_device, self.control, self.betas[0], self.betas[1], self.eps,
-                            self.max_grad_norm, self.workspace, stream=stream)
+        ql.qlora_adamw_step(self.plan, self._plan_ptr, self._control_ptr, self.betas[0], self.betas[1], self.eps,
+                            self.max_grad_norm, self._workspace_ptr, self._workspace_bytes, stream=stream)
 
     def grad_norm(self, out: torch.Tensor, grad_scale: Optional[float] = None, stream=None) -> None:
         """out [1] fp32: the norm of all gradients, times the grad_scale the optimizer was made with (or this one)."""
         self._here()
-        ql.qlora_grad_norm(self.plan, self.plan_device, self.grad_scale if grad_scale is None else grad_scale, out,
-                           self.workspace, stream=stream)
+        ql.qlora_grad_norm(self.plan, self._plan_ptr, self.grad_scale if grad_scale is None else grad_scale, out,
+                           self._workspace_ptr, self._workspace_bytes, stream=stream)
