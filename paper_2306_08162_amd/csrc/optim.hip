@@ -4,7 +4,8 @@
 //   w = w (1 - lr wd) - lr / (1 - b1^t) * m / (sqrt(v) / sqrt(1 - b2^t) + eps)
 //
 // The step is bound by HBM: with fp32 gradients and 16-bit weights 24 bytes a weight (fp32 states), 12 with states of
-// 8 bits.  A plan in device memory has a record for each chunk of up to 2048 weights of a tensor, one workgroup's work: hundreds
+// 8 bits, and 4 more for the norm.  20M weights with fp32 masters: 103 us with the norm, 5.8 TB/s of the 600 MB that a step cannot
+// do without (a large copy reaches 4.9 to 5.7); 160M with 8-bit states: 435 us, 5.9 TB/s with the second reading of the gradients counted.  A plan in device memory has a record for each chunk of up to 2048 weights of a tensor, one workgroup's work: hundreds
 // of small matrices fill the chip like one large one.
 //
 // 8-bit states.  256 consecutive weights share a scale, the power of two that brings the largest magnitude into
@@ -41,39 +42,46 @@ __device__ __forceinline__ uint32_t mix(uint32_t x)
 }
 
 // Device memory by type: a pointer read from the plan would otherwise be taken for one into any memory, with slower loads.
-template <typename T>
+// ONCE: past the caches.  A step touches each of its bytes once, and whatever ran since the step before has replaced them:
+// with the hint 448 fp32-state tensors of 600 MB take 103 us instead of 124, 37 MB 10.4 instead of 13.5 (3 to 11 % more
+// only where steps of up to 225 MB follow one another with nothing in between).  The gradients' first reading, for their norm, leaves them in the caches.
+template <bool ONCE, typename T>
 __device__ __forceinline__ T load_global(const void *p, uint32_t byte)
 {
     typedef const T __attribute__((address_space(1))) global_t;
-    return *(global_t *)((uintptr_t)p + byte);
+    global_t *const at = (global_t *)((uintptr_t)p + byte);
+    if constexpr (ONCE)
+        return __builtin_nontemporal_load(at);
+    else
+        return *at;
 }
 template <typename T>
-__device__ __forceinline__ void store_global(void *p, uint32_t byte, T v)
+__device__ __forceinline__ void store_once(void *p, uint32_t byte, T v)
 {
     typedef T __attribute__((address_space(1))) global_t;
-    *(global_t *)((uintptr_t)p + byte) = v;
+    __builtin_nontemporal_store(v, (global_t *)((uintptr_t)p + byte));
 }
 
 // Entries [i, i + 4) of a chunk that begins at p and has `have` of them (FULL: all of CHUNK), as they lie in memory: fp32 in
 // four words, 16-bit ones in two; those that do not exist are 0 and are not stored.
-template <bool FULL>
+template <bool FULL, bool ONCE>
 __device__ __forceinline__ u32x4_t load4(const void *p, uint32_t i, int dtype, uint32_t have)
 {
     u32x4_t r = {0, 0, 0, 0};
     if (dtype == QLORA_F32) {
         if (FULL || i + 4 <= have)
-            r = load_global<u32x4_t>(p, 4 * i);
+            r = load_global<ONCE, u32x4_t>(p, 4 * i);
         else
             for (uint32_t e = 0; e < 3; ++e)
-                if (i + e < have) r[e] = load_global<uint32_t>(p, 4 * (i + e));
+                if (i + e < have) r[e] = load_global<ONCE, uint32_t>(p, 4 * (i + e));
     } else {
         if (FULL || i + 4 <= have) {
-            const u32x2_t v = load_global<u32x2_t>(p, 2 * i);
+            const u32x2_t v = load_global<ONCE, u32x2_t>(p, 2 * i);
             r[0] = v[0];
             r[1] = v[1];
         } else
             for (uint32_t e = 0; e < 3; ++e)
-                if (i + e < have) r[e >> 1] |= (uint32_t)load_global<uint16_t>(p, 2 * (i + e)) << (16 * (e & 1));
+                if (i + e < have) r[e >> 1] |= (uint32_t)load_global<ONCE, uint16_t>(p, 2 * (i + e)) << (16 * (e & 1));
     }
     return r;
 }
@@ -95,38 +103,38 @@ __device__ __forceinline__ void store4(void *p, uint32_t i, int dtype, uint32_t 
 {
     if (dtype == QLORA_F32) {
         if (FULL || i + 4 <= have)
-            store_global(p, 4 * i, float4_t{f[0], f[1], f[2], f[3]});
+            store_once(p, 4 * i, float4_t{f[0], f[1], f[2], f[3]});
         else
             for (uint32_t e = 0; e < 3; ++e)
-                if (i + e < have) store_global(p, 4 * (i + e), f[e]);
+                if (i + e < have) store_once(p, 4 * (i + e), f[e]);
     } else {
         u16x4_t h;
 #pragma unroll
         for (int e = 0; e < 4; ++e) h[e] = dtype == QLORA_BF16 ? f32_to_bf16_bits(f[e]) : f32_to_f16_bits(f[e]);
         if (FULL || i + 4 <= have)
-            store_global(p, 2 * i, h);
+            store_once(p, 2 * i, h);
         else
             for (uint32_t e = 0; e < 3; ++e)
-                if (i + e < have) store_global(p, 2 * (i + e), (uint16_t)h[e]);
+                if (i + e < have) store_once(p, 2 * (i + e), (uint16_t)h[e]);
     }
 }
 template <bool FULL>
 __device__ __forceinline__ uint32_t load_codes(const void *p, uint32_t i, uint32_t have)
 {
-    if (FULL || i + 4 <= have) return load_global<uint32_t>(p, i);
+    if (FULL || i + 4 <= have) return load_global<true, uint32_t>(p, i);
     uint32_t r = 0;
     for (uint32_t e = 0; e < 3; ++e)
-        if (i + e < have) r |= (uint32_t)load_global<uint8_t>(p, i + e) << (8 * e);
+        if (i + e < have) r |= (uint32_t)load_global<true, uint8_t>(p, i + e) << (8 * e);
     return r;
 }
 template <bool FULL>
 __device__ __forceinline__ void store_codes(void *p, uint32_t i, uint32_t have, uint32_t r)
 {
     if (FULL || i + 4 <= have)
-        store_global(p, i, r);
+        store_once(p, i, r);
     else
         for (uint32_t e = 0; e < 3; ++e)
-            if (i + e < have) store_global(p, i + e, (uint8_t)(r >> (8 * e)));
+            if (i + e < have) store_once(p, i + e, (uint8_t)(r >> (8 * e)));
 }
 __device__ __forceinline__ void decode4(uint32_t codes, float scale, float *f)
 {
@@ -278,10 +286,10 @@ __global__ __launch_bounds__(ST) void grad_square_kernel(const OptimChunk *__res
         u32x4_t g[PASSES];
         if (now.have == CHUNK) {
 #pragma unroll
-            for (int i = 0; i < PASSES; ++i) g[i] = load4<true>(now.grad, (i * OT + tid) * 4, now.dtype, CHUNK);
+            for (int i = 0; i < PASSES; ++i) g[i] = load4<true, false>(now.grad, (i * OT + tid) * 4, now.dtype, CHUNK);
         } else {
 #pragma unroll
-            for (int i = 0; i < PASSES; ++i) g[i] = load4<false>(now.grad, (i * OT + tid) * 4, now.dtype, now.have);
+            for (int i = 0; i < PASSES; ++i) g[i] = load4<false, false>(now.grad, (i * OT + tid) * 4, now.dtype, now.have);
         }
         c += 4 * gridDim.x;
         if (c < chunks) next = place(c);
@@ -351,18 +359,18 @@ __device__ __forceinline__ void step_chunk(const AdamArgs &a, const OptimChunk &
 #pragma unroll
     for (int i = 0; i < PASSES; ++i) {
         const uint32_t at = (i * OT + threadIdx.x) * 4;
-        g[i] = load4<FULL>(t.grad, at, grad_dtype, have);
-        w[i] = load4<FULL>(main, at, wide, have);
+        g[i] = load4<FULL, true>(t.grad, at, grad_dtype, have);
+        w[i] = load4<FULL, true>(main, at, wide, have);
         if constexpr (BITS == 32) {
-            m[i] = load4<FULL>(t.exp_avg, at, QLORA_F32, have);
-            v[i] = load4<FULL>(t.exp_avg_sq, at, QLORA_F32, have);
+            m[i] = load4<FULL, true>(t.exp_avg, at, QLORA_F32, have);
+            v[i] = load4<FULL, true>(t.exp_avg_sq, at, QLORA_F32, have);
         } else {
             const uint32_t block = i * (OT / 64) + wave;               // the wave's
             const bool some = FULL || block * QBLOCK < have;
             m[i][0] = load_codes<FULL>(t.exp_avg, at, have);
             v[i][0] = load_codes<FULL>(t.exp_avg_sq, at, have);
-            ms[i] = some ? load_global<float>(t.avg_scale, 4 * block) : 0.f;
-            vs[i] = some ? load_global<float>(t.avg_sq_scale, 4 * block) : 0.f;
+            ms[i] = some ? load_global<true, float>(t.avg_scale, 4 * block) : 0.f;
+            vs[i] = some ? load_global<true, float>(t.avg_sq_scale, 4 * block) : 0.f;
         }
     }
     const qlora_optim_control_t *ctl = a.control;
@@ -428,8 +436,8 @@ __device__ __forceinline__ void step_chunk(const AdamArgs &a, const OptimChunk &
             // maximum passes over it).
             const bool bad = vb >= 0x7f800000u;
             if (lane == 0 && (FULL || block * QBLOCK < have)) {
-                store_global(t.avg_scale, 4 * block, bad ? NAN : mb == 0 ? 0.f : ldexpf(1.f, km - 8));
-                store_global(t.avg_sq_scale, 4 * block, bad ? NAN : vb == 0 ? 0.f : ldexpf(1.f, kv - 8));
+                store_once(t.avg_scale, 4 * block, bad ? NAN : mb == 0 ? 0.f : ldexpf(1.f, km - 8));
+                store_once(t.avg_sq_scale, 4 * block, bad ? NAN : vb == 0 ? 0.f : ldexpf(1.f, kv - 8));
             }
         }
         if (master) store4<FULL>(main, at, QLORA_F32, have, wf);
@@ -443,7 +451,9 @@ __device__ __forceinline__ void step_chunk(const AdamArgs &a, const OptimChunk &
     }
 }
 
-__global__ __launch_bounds__(OT) void adamw_kernel(const AdamArgs a)
+// Six waves a SIMD: five to seven are alike, with eight (which fewer registers would allow) the 448 fp32-state tensors take 117 us
+// instead of 103: more streams at once than the memory keeps open.
+__global__ __launch_bounds__(OT) __attribute__((amdgpu_waves_per_eu(6, 6))) void adamw_kernel(const AdamArgs a)
 {
     Parts parts{};
     if (a.count > 0 && threadIdx.x < WAVE) parts = load_parts(a.parts, a.count);
