@@ -383,7 +383,8 @@ int qlora_lrec_loss_scaled(const void *student_logits, const void *teacher_logit
  * token -1 and -inf).  A row that masks every token has log p = -inf everywhere, entropy 0 and no alternatives.  A NaN
  * or plus infinity in a row makes its logprob, entropy, alt_logprobs and stats NaN and its alt_tokens -1.
  *
- * logits and stats are 16-byte aligned, the other pointers 4; V >= 1, M < 2^22, M*V < 2^35, M*row_stride < 2^40.
+ * logits may begin at any element (a slice of a larger tensor), stats is 16-byte aligned, the other pointers 4; V <= 2^28,
+ * M < 2^22, M*V < 2^35, M*row_stride < 2^40.
  * workspace: qlora_token_logprobs_workspace_bytes(M, V, alternatives, dtype) bytes; NULL is accepted where that is 0
  * because rows are short (a call with bad arguments says so itself).  Sums run in a fixed order: results are bitwise
  * reproducible.

@@ -768,7 +768,7 @@ namespace {
 
 int check_logits(int M, int V, int dtype)
 {
-    if (M < 1 || V < 1 || M >= (1 << 22) || (long long)M * V >= (1ll << 35)) return QLORA_E_SHAPE;
+    if (M < 1 || V < 1 || M >= (1 << 22) || V > (1 << 28) || (long long)M * V >= (1ll << 35)) return QLORA_E_SHAPE;
     if (dtype != QLORA_F16 && dtype != QLORA_BF16 && dtype != QLORA_F32) return QLORA_E_DTYPE;
     return QLORA_OK;
 }
@@ -777,6 +777,8 @@ int check_stride(int M, int V, int64_t stride)
     return stride < V || stride >= (1ll << 40) || stride * M >= (1ll << 40) ? QLORA_E_VALUE : QLORA_OK;
 }
 inline bool odd4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
+inline size_t dtype_bytes(int dtype) { return dtype == QLORA_F32 ? 4 : 2; }
+inline bool between_elements(const void *p, int dtype) { return reinterpret_cast<uintptr_t>(p) % dtype_bytes(dtype) != 0; }
 
 }  // namespace
 
@@ -798,7 +800,7 @@ int qlora_token_logprobs(const void *logits, int64_t row_stride, const int32_t *
     if (!logits || (logprob && !tokens) || (alternatives > 0 && (!alt_tokens || !alt_logprobs)) ||
         (!logprob && !entropy && !stats && alternatives == 0))
         return QLORA_E_NULL;
-    if (misaligned(logits) || misaligned(stats) || misaligned(workspace) || odd4(tokens) || odd4(logprob) || odd4(entropy) ||
+    if (between_elements(logits, dtype) || misaligned(stats) || misaligned(workspace) || odd4(tokens) || odd4(logprob) || odd4(entropy) ||
         (alternatives > 0 && (odd4(alt_tokens) || odd4(alt_logprobs))))
         return QLORA_E_ALIGN;
     const size_t need = qlora_token_logprobs_workspace_bytes(M, V, alternatives, dtype);
@@ -818,7 +820,7 @@ int qlora_token_logprobs_bwd(const void *logits, int64_t row_stride, const int32
     if ((st = check_stride(M, V, row_stride)) != QLORA_OK || (st = check_stride(M, V, d_row_stride)) != QLORA_OK) return st;
     if (dlogits == logits && d_row_stride != row_stride && M > 1) return QLORA_E_VALUE;
     if (!logits || !stats || !dlogits || (!d_logprob && !d_entropy) || (d_logprob && !tokens)) return QLORA_E_NULL;
-    if (misaligned(logits) || misaligned(stats) || misaligned(dlogits) || odd4(tokens) || odd4(d_logprob) || odd4(d_entropy))
+    if (between_elements(logits, dtype) || misaligned(stats) || between_elements(dlogits, dtype) || odd4(tokens) || odd4(d_logprob) || odd4(d_entropy))
         return QLORA_E_ALIGN;
     begin_call();
     launch_token_logprobs_bwd(logits, row_stride, tokens, stats, d_logprob, d_entropy, dlogits, d_row_stride, M, V, dtype,
@@ -834,7 +836,6 @@ struct Range {
 };
 
 inline bool beta_ok(double b) { return b >= 0.0 && b < 1.0; }
-inline size_t dtype_bytes(int dtype) { return dtype == QLORA_F32 ? 4 : 2; }
 
 // total weights, blocks and chunks of a set of tensors; false: a number out of range
 bool count_weights(int count, const qlora_optim_tensor_t *tensors, uint64_t &weights, uint64_t &blocks, uint64_t &chunks)

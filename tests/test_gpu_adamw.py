@@ -58,7 +58,7 @@ class _Set:
             for n in ("exp_avg", "exp_avg_sq", "avg_scale", "avg_sq_scale"):
                 if n in self.buf:
                     self.put(n, i, np.zeros(self.length(n, i)))
-            self.gradient(0)
+        self.gradient(0)
         self.start = {n: b.clone() for n, b in self.buf.items()}
 
     def length(self, name, i):
@@ -453,3 +453,27 @@ def test_adapters_learn_from_token_scores():
 
 def _host16(t):
     return t.cpu().numpy().view(np.uint16)
+
+
+def test_tensor_of_more_than_two_to_the_31_weights():
+    """Offsets that pass 32 bits: bf16 weights and gradients with 8-bit states, gradients at both ends and at 2^31."""
+    import torch
+    from paper_2306_08162_amd.device import AdapterOptimizer, OptimTensor
+    announce("adamw, one tensor of 2^31 + 5001 weights")
+    n = 2 ** 31 + 5001
+    new = lambda size, t: torch.zeros(size, dtype=t, device="cuda:0")
+    w, g = new(n, torch.bfloat16), new(n, torch.bfloat16)
+    places = [slice(0, 300), slice(2 ** 31 - 5, 2 ** 31 + 7), slice(n - 300, n)]
+    for s in places:
+        g[s] = 0.5
+    opt = AdapterOptimizer([OptimTensor(w, g, state_bits=8)], lr=1e-2, max_grad_norm=1e3)
+    opt.step()
+    count = sum(s.stop - s.start for s in places)
+    assert abs(float(opt.last_grad_norm) - 0.5 * np.sqrt(count)) <= 2 * U * 0.5 * np.sqrt(count)
+    for s in places:                     # a first step moves each weight by lr against its gradient
+        assert (w[s].float() + 1e-2).abs().max() <= 1e-2 * 2 ** -8
+    moved = 0
+    for at in range(0, n, 2 ** 28):      # ... and no other weight
+        moved += int((w[at:at + 2 ** 28] != 0).sum())
+    assert moved == count
+    assert int((opt.tensors[0].exp_avg[n - 300:] != 0).sum()) == 300 and int((opt.tensors[0].exp_avg_sq[:300] != 0).sum()) == 300

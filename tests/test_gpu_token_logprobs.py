@@ -98,14 +98,14 @@ class _Call:
         worst = np.max(np.abs(got[ok] - want[ok]) / np.broadcast_to(bound, want.shape)[ok]) if ok.any() else 0.0
         assert worst <= 1.0, f"{worst:.3g} times the bound"
 
-    def backward(self, g, h, d_pad=0, into=None, stream=None):
+    def backward(self, g, h, d_pad=0, into=None, stride=None, stream=None):
         import torch
         M, V = self.shape
         up = lambda a: None if a is None else torch.from_numpy(np.asarray(a, np.float32)).to("cuda:0")
         self.g, self.h = up(g), up(h)
         self.dlogits = torch.full((M, V + d_pad), 55, dtype=_torch(self.dtype), device="cuda:0") if into is None else into
         ql.qlora_token_logprobs_bwd(self.logits, V + self.pad, self.tokens, self.stats, self.g, self.h, self.dlogits,
-                                    self.dlogits.shape[1], M, V, FLAG[self.dtype], stream=stream)
+                                    stride or self.dlogits.shape[1], M, V, FLAG[self.dtype], stream=stream)
 
     def check_gradient(self):
         M, V = self.shape
@@ -143,6 +143,9 @@ SHAPES = [
     (2, 32003, "bf16", 20, 61), (2, 32768, "f16", 64, 0), (2, 32769, "f16", 20, 0), (3, 16384, "f32", 20, 0),
     (2, 16385, "f32", 64, 0), (2, 50257, "f32", 8, 1), (2, 128259, "bf16", 20, 61), (1, 400001, "f16", 16, 0),
     (70, 999, "f16", 3, 0), (33, 32000, "f32", 20, 0),
+    # more rows than compute units: other workgroups (64 to 512 threads), rows in one piece and in segments
+    (300, 400, "f16", 5, 0), (1100, 3001, "bf16", 64, 1), (2100, 5000, "f16", 2, 0), (260, 31999, "f16", 20, 0),
+    (258, 40001, "bf16", 33, 3), (90, 128259, "bf16", 20, 61), (130, 40000, "f32", 5, 0),
 ]
 
 
@@ -159,10 +162,10 @@ def test_scores_and_gradient(M, V, dtype, k, pad):
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
-@pytest.mark.parametrize("V", [100, 5000, 40000])
-def test_masks(V, dtype):
+@pytest.mark.parametrize("V,times", [(100, 1), (5000, 1), (40000, 1), (5000, 30), (20000, 30)])
+def test_masks(V, times, dtype):
     """Rows that mask all, all but one, all but a few, by -inf and by the type's lowest number; a masked target."""
-    announce(f"token logprobs masks V={V} {dtype}")
+    announce(f"token logprobs masks V={V} {dtype}, {times} times")
     import torch
     low = torch.finfo(_torch(dtype)).min
     M = 10
@@ -179,6 +182,7 @@ def test_masks(V, dtype):
     z[8, ::3] = low
     tokens = _tokens(V + 1, M, V)
     tokens[:9] = [V, 0, few[0], 1, few[0], few[1], few[2], V - 1, 3]
+    z, tokens, M = np.tile(z, (times, 1)), np.tile(tokens, times), M * times
     for k in (8, 20, 64):
         c = _Call(z, tokens, dtype, k)
         c.forward()
@@ -189,7 +193,8 @@ def test_masks(V, dtype):
 
 @pytest.mark.parametrize("dtype", ["f16", "f32"])
 @pytest.mark.parametrize("kind", ["rising", "falling", "constant", "two_values", "hot_run", "integers", "zeros_of_both_signs"])
-def test_alternatives_of_rows_in_order(kind, dtype):
+@pytest.mark.parametrize("times", [1, 131])
+def test_alternatives_of_rows_in_order(kind, dtype, times):
     """Rows that defeat the first threshold: more entries above it than fit, and ties that go to the lower index."""
     announce(f"token logprobs alternatives {kind} {dtype}")
     M, V = 2, 20000
@@ -197,9 +202,9 @@ def test_alternatives_of_rows_in_order(kind, dtype):
     row = {"rising": i / 4096.0, "falling": -i / 4096.0, "constant": np.full(V, 1.5), "two_values": np.where(i % 7001 == 5, 2.0, 1.0),
            "hot_run": np.where((i > 3000) & (i < 9000), 5.0 + (i % 997) / 512.0, -3.0),
            "integers": (i * 7919 % 23).astype(float), "zeros_of_both_signs": np.where(i % 2 == 0, -0.0, 0.0)}[kind]
-    z = _rounded(np.stack([row, row[::-1]]), dtype)
-    for k in (1, 5, 8, 33, 64):
-        c = _Call(z, [3, V - 2], dtype, k)
+    z = np.tile(_rounded(np.stack([row, row[::-1]]), dtype), (times, 1))
+    for k in (1, 5, 8, 33, 64) if times == 1 else (1, 20, 64):
+        c = _Call(z, [3, V - 2] * times, dtype, k)
         c.forward()
         c.check()
 
@@ -259,6 +264,36 @@ def test_outputs_are_optional():
         assert torch.equal(getattr(c, only), getattr(full, only))
         if only == "alt":
             assert torch.equal(c.alt_lp, full.alt_lp)
+
+
+@pytest.mark.parametrize("dtype,offset", [("f16", 1), ("f16", 5), ("bf16", 3), ("f32", 1), ("f32", 3)])
+def test_slices_of_larger_tensors(dtype, offset):
+    """The last position of every sequence of a batch with an odd vocabulary: rows begin at any element, S V apart."""
+    import torch
+    announce(f"token logprobs slices {dtype} {offset}")
+    batch, S, V, k = 5, 3, 3001, 9
+    whole = _logits(60, batch * S, V, dtype)
+    store = torch.zeros(batch * S * V + offset, dtype=_torch(dtype), device="cuda:0")
+    store[offset:] = _upload(whole, dtype, 0).view(-1)
+    z = whole.reshape(batch, S, V)[:, -1]
+    c = _Call(z, _tokens(61, batch, V), dtype, k)
+    c.logits, c.pad = store[offset:].view(batch, S, V)[:, -1], (S - 1) * V
+    c.forward()
+    c.check()
+    d = torch.full((batch * S * V + offset,), 55, dtype=_torch(dtype), device="cuda:0")
+    c.backward(np.linspace(-1, 2, batch), np.ones(batch), into=d[offset:].view(batch, S, V)[:, -1], stride=S * V)
+    c.check_gradient()
+    others = d[offset:].view(batch, S, V)[:, :-1].float()
+    assert (others == 55).all() and (d[:offset].float() == 55).all()
+
+
+def test_entropy_gradient_without_tokens():
+    announce("token logprobs, entropy alone")
+    c = _Call(_logits(80, 4, 1000, "f16"), [-1] * 4, "f16", 0)
+    c.forward()
+    c.tokens = None
+    c.backward(None, [1.0, 0.0, -2.0, 0.5])
+    c.check_gradient()
 
 
 @pytest.mark.parametrize("dtype", ["f16", "f32"])
@@ -336,3 +371,30 @@ def test_graph_replays_match_eager():
         torch.cuda.synchronize()
         for a, b in zip(eager[rep % 3], outs()):
             assert torch.equal(a, b), f"replay {rep}"
+
+
+def test_logits_beyond_four_gigabytes():
+    """Offsets that pass 32 bits, of elements and of bytes: sampled rows of 70000 x 32000, scored and differentiated in place."""
+    import torch
+    announce("token logprobs 70000 x 32000 f16")
+    M, V, k = 70000, 32000, 3
+    dev = "cuda:0"
+    z = torch.empty((M, V), dtype=torch.float16, device=dev)
+    part = torch.randn((1000, V), device=dev, generator=torch.Generator(device=dev).manual_seed(5)).mul_(2.5).half()
+    for at in range(0, M, 1000):
+        z[at:at + 1000] = part.roll(at // 1000 * 37, 1)
+    tokens = (torch.arange(M, device=dev) * 7919 % V).int()
+    new = lambda *s, t=torch.float32: torch.empty(s, dtype=t, device=dev)
+    lp, H, st, alt, alp, g = new(M), new(M), new(M, 4), new(M, k, t=torch.int32), new(M, k), torch.ones(M, device=dev)
+    rows = np.array([0, 1, 33554, 33555, 67107, 67109, 67110, M - 2, M - 1])
+    zs = z[torch.from_numpy(rows).to(dev)].double().cpu().numpy()
+    ql.qlora_token_logprobs(z, V, tokens, lp, H, alt, alp, k, st, M, V, ql.QLORA_F16, None)
+    ql.qlora_token_logprobs_bwd(z, V, tokens, st, g, None, z, V, M, V, ql.QLORA_F16)
+    at = torch.from_numpy(rows).to(dev)
+    ts = tokens[at].cpu().numpy()
+    wl_, wH, walt, walp = scoring.score(zs, ts, k)
+    np.testing.assert_allclose(lp[at].cpu().numpy(), wl_, atol=C * U * 40)
+    np.testing.assert_allclose(H[at].cpu().numpy(), wH, atol=C * U * 40)
+    np.testing.assert_array_equal(alt[at].cpu().numpy(), walt)
+    dz = scoring.score_gradient(zs, ts, np.ones(len(rows)), None)
+    np.testing.assert_allclose(z[at].double().cpu().numpy(), dz, rtol=2 * HALF_ULP["f16"], atol=TINY["f16"] * 1.01)

@@ -23,7 +23,8 @@ def _score(z=FAKE, stride=64, tok=FAKE, lp=FAKE, ent=FAKE, at=FAKE, alp=FAKE, k=
     (dict(k=-1), "VALUE"), (dict(k=65), "VALUE"),
     (dict(z=None), "NULL"), (dict(tok=None), "NULL"), (dict(at=None), "NULL"), (dict(alp=None), "NULL"),
     (dict(lp=None, ent=None, stats=None, k=0), "NULL"),
-    (dict(z=ODD), "ALIGN"), (dict(stats=ODD), "ALIGN"), (dict(ws=ODD), "ALIGN"), (dict(tok=0x10002), "ALIGN"),
+    (dict(z=0x10001), "ALIGN"), (dict(z=0x10002, dtype=2), "ALIGN"), (dict(stats=ODD), "ALIGN"), (dict(ws=ODD), "ALIGN"),
+    (dict(tok=0x10002), "ALIGN"), (dict(V=(1 << 28) + 1, M=1, stride=1 << 29), "SHAPE"),
     (dict(lp=0x10002), "ALIGN"), (dict(ent=0x10001), "ALIGN"), (dict(at=0x10002), "ALIGN"), (dict(alp=0x10002), "ALIGN"),
     (dict(V=1 << 20, stride=1 << 20, ws=None), "WORKSPACE"), (dict(V=1 << 20, stride=1 << 20, wsb=64), "WORKSPACE"),
 ])
@@ -41,7 +42,8 @@ def test_token_logprobs_workspace():
 @pytest.mark.parametrize("change,status", [
     (dict(M=0), "SHAPE"), (dict(V=0), "SHAPE"), (dict(dtype=3), "DTYPE"), (dict(stride=63), "VALUE"), (dict(ds=63), "VALUE"),
     (dict(z=None), "NULL"), (dict(stats=None), "NULL"), (dict(dz=None), "NULL"), (dict(g=None, h=None), "NULL"),
-    (dict(tok=None), "NULL"), (dict(z=ODD), "ALIGN"), (dict(dz=ODD), "ALIGN"), (dict(stats=ODD), "ALIGN"),
+    (dict(tok=None), "NULL"), (dict(z=0x10001), "ALIGN"), (dict(dz=0x20001), "ALIGN"), (dict(stats=ODD), "ALIGN"),
+    (dict(dz=0x20002, dtype=2), "ALIGN"),
     (dict(g=0x10002), "ALIGN"), (dict(h=0x10002), "ALIGN"), (dict(tok=0x10002), "ALIGN"), (dict(dz=FAKE, ds=65), "VALUE"),
 ])
 def test_token_logprobs_bwd_refusals(change, status):
