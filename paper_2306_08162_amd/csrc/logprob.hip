@@ -267,7 +267,8 @@ __global__ __launch_bounds__(PT) void score_kernel(const ScoreArgs a)
         if (a.k > 0) {
             const int rank = (a.k + waves - 1) / waves;
             const uint32_t mine = order_of(mx);
-            uint32_t l = order_of(wave_least(mx)), h = order_of(hi);
+            uint32_t l = __builtin_amdgcn_readfirstlane(order_of(wave_least(mx))),
+                     h = __builtin_amdgcn_readfirstlane(order_of(hi));
             int reach = rank == 1 ? 1 : 64;                            // so many lanes reach l
             for (int i = 0; i < 12 && reach > rank + rank / 4 && h - l > 1; ++i) {
                 const uint32_t mid = l + (h - l) / 2;
@@ -469,24 +470,22 @@ __global__ __launch_bounds__(PT) void score_kernel(const ScoreArgs a)
     }
 }
 
-// joins the segments of a row; one wave a row
-constexpr int JOIN_KEYS = 256;
+// Joins the segments of a row.  Each wave joins the sums for itself; with alternatives four waves place the lists' keys.
+constexpr int JOIN_T = 256;
 template <int DT>
-__global__ __launch_bounds__(64) void score_join_kernel(const ScoreArgs a)
+__global__ __launch_bounds__(JOIN_T) void score_join_kernel(const ScoreArgs a)
 {
-    __shared__ key_t keys[QLORA_MAX_ALTERNATIVES + JOIN_KEYS];         // the best so far, and the next lists' keys
-    const int row = blockIdx.x, lane = threadIdx.x;
-    const float4_t *part = a.part + (long)row * a.splits;
+    __shared__ key_t keys[QLORA_MAX_ALTERNATIVES + JOIN_T];            // the best so far, and the next lists' keys
+    const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
     const int token = a.logprob ? a.token[row] : -1;
-    const bool given = token >= 0 && token < a.V;
-    const float zt = given ? logit_at<DT>((const char *)a.z + (long)row * a.stride * (DT == 2 ? 4 : 2), token) : NAN;
+    const float4_t *part = a.part + (long)row * a.splits;
     float4_t v = {-INFINITY, 0.f, 0.f, 0.f};
     if (lane < a.splits) v = part[lane];
     const key_t *lists = a.lists + (long)row * a.splits * a.k;
     const int all = a.splits * a.k;
-    key_t first[JOIN_KEYS / 64];                                       // requested with the rest
-#pragma unroll
-    for (int c = 0; c < JOIN_KEYS / 64; ++c) first[c] = lane + 64 * c < all ? lists[lane + 64 * c] : 0;
+    key_t next = tid < all ? lists[tid] : 0;                           // requested with the rest
+    const bool given = token >= 0 && token < a.V;
+    const float zt = given ? logit_at<DT>((const char *)a.z + (long)row * a.stride * (DT == 2 ? 4 : 2), token) : NAN;
     float m = v[0];
     bool bad = v[2] != v[2];
     for (int i = lane + 64; i < a.splits; i += 64) {
@@ -514,40 +513,29 @@ __global__ __launch_bounds__(64) void score_join_kernel(const ScoreArgs a)
     s = wave_total(s);
     q = wave_total(q);
     const float lt = poison ? NAN : m == -INFINITY ? 0.f : log_total(n, s);
-    if (lane == 0) write_row(a, row, given, zt, poison ? NAN : m, n, s, poison ? NAN : q, lt);
+    if (tid == 0) write_row(a, row, given, zt, poison ? NAN : m, n, s, poison ? NAN : q, lt);
     if (a.k == 0) return;
     int best = 0;                                                      // keys [0, best) are the best so far, in order
-    for (int at = 0; at < all; at += JOIN_KEYS) {
-        const int more = all - at < JOIN_KEYS ? all - at : JOIN_KEYS, have = best + more;
-#pragma unroll
-        for (int c = 0; c < JOIN_KEYS / 64; ++c)
-            if (lane + 64 * c < more) keys[best + lane + 64 * c] = at == 0 ? first[c] : lists[at + lane + 64 * c];
+    for (int at = 0; at < all; at += JOIN_T) {
+        const int have = best + (all - at < JOIN_T ? all - at : JOIN_T);
+        if (best + tid < have) keys[best + tid] = next;
         __syncthreads();
-        key_t mine[(QLORA_MAX_ALTERNATIVES + JOIN_KEYS) / 64];
-        int place[(QLORA_MAX_ALTERNATIVES + JOIN_KEYS) / 64];
-#pragma unroll
-        for (int c = 0; c < (QLORA_MAX_ALTERNATIVES + JOIN_KEYS) / 64; ++c) {
-            const int i = lane + 64 * c;
-            mine[c] = i < have ? keys[i] : 0;
-            place[c] = mine[c] ? 0 : a.k;                              // key 0: a place that a short list left open
-        }
+        if (at + JOIN_T + tid < all) next = lists[at + JOIN_T + tid];
+        // a key's place is the number of larger ones; key 0 is a place that a short list left open
+        const key_t low = tid < have ? keys[tid] : 0, high = JOIN_T + tid < have ? keys[JOIN_T + tid] : 0;
+        int low_place = 0, high_place = 0;
 #pragma unroll 4
         for (int j = 0; j < have; ++j) {
-            const key_t other = keys[j];
-#pragma unroll
-            for (int c = 0; c < (QLORA_MAX_ALTERNATIVES + JOIN_KEYS) / 64; ++c) place[c] += other > mine[c];
+            low_place += keys[j] > low;
+            high_place += keys[j] > high;
         }
-        __syncthreads();
-        int held = 0;
-#pragma unroll
-        for (int c = 0; c < (QLORA_MAX_ALTERNATIVES + JOIN_KEYS) / 64; ++c) {
-            if (place[c] < a.k) keys[place[c]] = mine[c];
-            held += __popcll(__ballot(place[c] < a.k));
-        }
-        best = held;
+        const int kept = __syncthreads_count(low != 0) + __syncthreads_count(high != 0);
+        if (low && low_place < a.k) keys[low_place] = low;
+        if (high && high_place < a.k) keys[high_place] = high;
+        best = kept < a.k ? kept : a.k;
         __syncthreads();
     }
-    for (int i = lane; i < a.k; i += 64) write_alternative(a, row, i, i < best ? keys[i] : 0, m, lt, poison);
+    if (tid < a.k) write_alternative(a, row, tid, tid < best ? keys[tid] : 0, m, lt, poison);
 }
 
 struct ScoreGradArgs {
@@ -651,7 +639,7 @@ void launch_score(const ScoreArgs &a, const ScorePlan &p, hipStream_t s)
         else
             QLORA_LAUNCH((score_kernel<DT, false, MANY_PT, MANY_PCH>), grid, block, 0, s, a);
     }
-    if (a.splits > 1) QLORA_LAUNCH((score_join_kernel<DT>), dim3(a.M), dim3(64), 0, s, a);
+    if (a.splits > 1) QLORA_LAUNCH((score_join_kernel<DT>), dim3(a.M), dim3(a.k > 0 ? JOIN_T : WAVE), 0, s, a);
 }
 
 }  // namespace
