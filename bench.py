@@ -354,6 +354,84 @@ def run_lrec_loss(M: int = 2048, V: int = 32000, iters: int = 20):
             "plain_copy_GBps_same_box": round(copy_gbps, 1), "loss_mean": float(mean.cpu()[0])}
 
 
+def _us_per_call(call, iters):
+    """Mean time of call(0), call(1), ... on the GPU, after as many untimed ones (the clocks take milliseconds to come up)."""
+    import torch
+    from paper_2306_08162_amd.hiprt import Event
+    for i in range(iters):
+        call(i)
+    torch.cuda.synchronize()
+    stream = torch.cuda.current_stream().cuda_stream or None
+    e0, e1 = Event(), Event()
+    e0.record(stream)
+    for i in range(iters):
+        call(i)
+    e1.record(stream)
+    e1.synchronize()
+    return e0.elapsed_ms(e1) * 1e3 / iters
+
+
+def run_token_logprobs(M: int = 2048, V: int = 32000, iters: int = 50):
+    """Scoring of M given tokens over a LLaMA vocabulary, alone, with 20 alternatives, and with the gradient of a policy
+    objective (entropy included).  HBM-bound; four sets of logits are rotated (131 MB each)."""
+    import torch
+    from paper_2306_08162_amd import binding as ql
+    dev = torch.device("cuda:0")
+    g = torch.Generator(device=dev)
+    g.manual_seed(0x10554)
+    logits = [torch.randn((M, V), device=dev, generator=g).mul_(2.5).half() for _ in range(4)]
+    tokens = torch.randint(0, V, (M,), dtype=torch.int32, device=dev, generator=g)
+    f32 = lambda *shape: torch.empty(shape, device=dev)
+    logprob, entropy, stats, alt_lp, advantage = f32(M), f32(M), f32(M, 4), f32(M, 20), f32(M).fill_(8.0)
+    alt = torch.empty((M, 20), dtype=torch.int32, device=dev)
+    dlogits = torch.empty_like(logits[0])
+
+    def score(i, k=0, stats=None, entropy=None):
+        ql.qlora_token_logprobs(logits[i % 4], V, tokens, logprob, entropy, alt if k else None, alt_lp if k else None, k,
+                                stats, M, V, ql.QLORA_F16, None)
+
+    def step(i):
+        score(i, stats=stats, entropy=entropy)
+        ql.qlora_token_logprobs_bwd(logits[i % 4], V, tokens, stats, advantage, advantage, dlogits, V, M, V, ql.QLORA_F16)
+
+    nbytes = 2 * M * V
+    us = {"score": _us_per_call(score, iters), "score_20_alternatives": _us_per_call(lambda i: score(i, 20, None, entropy), iters),
+          "score_and_gradient": _us_per_call(step, iters)}
+    return {"workload": f"M={M} tokens x V={V} logits, fp16", "us_per_call": {k: round(v, 2) for k, v in us.items()},
+            "logit_bytes": nbytes, "score_GBps": round(nbytes / us["score"] * 1e-3, 1),
+            "mean_logprob": float(logprob.mean())}
+
+
+def run_adapter_optimizer(iters: int = 50):
+    """One clipped AdamW step over the adapters of every projection of LLaMA-7B: rank 8 with fp32 masters and states, rank 64
+    in bf16 with 8-bit states.  HBM-bound; every state is larger than the 256 MB last-level cache."""
+    import torch
+    from paper_2306_08162_amd import binding as ql
+    from paper_2306_08162_amd import workloads as wl
+    from paper_2306_08162_amd.device import AdapterOptimizer, OptimTensor
+    dev = torch.device("cuda:0")
+    g = torch.Generator(device=dev)
+    g.manual_seed(0x10555)
+    block = wl.config5(4, 16)
+    out = {}
+    for name, rank, dtype, bits, master in (("rank8_fp32_states", 8, torch.float16, 32, True),
+                                            ("rank64_8bit_states", 64, torch.bfloat16, 8, False)):
+        tensors, nbytes, count = [], 0, 0
+        for _ in range(32):
+            for c in block:
+                for size in (rank * c.K, c.N * rank):
+                    w = torch.randn(size, device=dev, generator=g).mul_(0.02)
+                    grad = torch.randn(size, device=dev, generator=g).mul_(1e-3)
+                    tensors.append(OptimTensor(w.to(dtype), grad, master=w if master else None, state_bits=bits))
+                    nbytes += size * (4 + (10 if master else 4) + bits // 2)
+                    count += size
+        opt = AdapterOptimizer(tensors, lr=2e-4, max_grad_norm=0.3, seed=1)
+        us = _us_per_call(lambda i: opt.step(), iters)
+        out[name] = {"tensors": len(tensors), "weights": count, "us_per_step": round(us, 2), "bytes_per_step": nbytes,
+                     "GBps": round(nbytes / us * 1e-3, 1), "grad_norm": float(opt.last_grad_norm)}
+    return out
+
+
 def run_actorder_gather(M: int = 2048, K: int = 4096, G: int = 128, iters: int = 20):
     """The run-time cost of an activation-order checkpoint: one column gather of x before the forward call and one
     of dX after the backward call (4 bytes per element each: read once, written once).  Eight buffers are rotated."""
@@ -561,6 +639,8 @@ def main() -> int:
         extras["small_m_M32"] = {"M": 32, "timing": "as small_m; two 16-row token blocks per weight fragment",
                                  **run_small_m(32, bit_widths=(2,), sibling_calls=False)}
         extras["lrec_loss"] = run_lrec_loss()
+        extras["token_logprobs"] = run_token_logprobs()
+        extras["adapter_optimizer"] = run_adapter_optimizer()
         extras["actorder_gather"] = run_actorder_gather()
         extras["stacked_adapters"] = run_stacked()
     cfg, layer, ms_per_step, fwd_ms, bwd_ms, diff_ms = run_headline(inp, args.steps, args.warmup)
