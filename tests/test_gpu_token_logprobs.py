@@ -245,16 +245,19 @@ def test_almost_certain_tokens_keep_their_digits():
     np.testing.assert_allclose(c.entropy.cpu().numpy(), H, rtol=300 * U)
 
 
-def test_outputs_are_optional():
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("M", [5, 300])
+def test_outputs_are_optional(M, dtype):
+    """Each output alone has the bits that it has beside the others."""
     import torch
-    announce("token logprobs optional outputs")
-    M, V, k = 5, 40000, 7
-    z, tokens = _logits(8, M, V, "bf16"), _tokens(8, M, V)
-    full = _Call(z, tokens, "bf16", k)
+    announce(f"token logprobs optional outputs M={M} {dtype}")
+    V, k = 30000, 7
+    z, tokens = _logits(8, M, V, dtype), _tokens(8, M, V)
+    full = _Call(z, tokens, dtype, k)
     full.forward()
     names = ("logprob", "entropy", "alt", "stats")
     for only in names:
-        c = _Call(z, tokens, "bf16", k if only == "alt" else 0)
+        c = _Call(z, tokens, dtype, k if only == "alt" else 0)
         for n in ("logprob", "entropy", "stats"):
             if n != only:
                 setattr(c, n, None)
