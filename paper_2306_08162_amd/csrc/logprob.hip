@@ -215,7 +215,8 @@ template <int DT, bool MOMENTS, int PT, int PCH>
 __global__ __launch_bounds__(PT) void score_kernel(const ScoreArgs a)
 {
     constexpr int E = Piece<DT>::E;
-    __shared__ float red[5][PT / 64];                  // of each wave: maximum, smallest group maximum; n, s, q
+    __shared__ float red[5][PT / 64];                  // of each wave: maximum, bound of its alternatives; n, s, q
+    __shared__ float log_s;
     __shared__ int hits, count, scan[PT / 64];
     __shared__ u32x4_t held[PCAP];                     // pieces with an entry above tau, and which they are
     __shared__ int held_at[PCAP];
@@ -352,12 +353,14 @@ __global__ __launch_bounds__(PT) void score_kernel(const ScoreArgs a)
     q = (q - slip * s) * exp2_hw(-slip);
     s *= exp2_hw(-slip);
     const bool poison = !(s < INFINITY) || m == INFINITY;
-    float lt = 0.f;
-    if (a.k > 0 || last_wave) lt = poison ? NAN : m == -INFINITY ? 0.f : log_total(n, s);
     if (a.splits > 1) {
         if (tid == 0) a.part[(long)row * a.splits + split] = float4_t{m, n, poison ? NAN : s, q};
-    } else if (tid == T - 64) {
-        write_row(a, row, given, zt, poison ? NAN : m, n, s, poison ? NAN : q, lt);
+    } else if (last_wave) {                            // the logarithm: a hundred instructions that one wave is enough for
+        const float lt = poison ? NAN : m == -INFINITY ? 0.f : log_total(n, s);
+        if (lane == 0) {
+            write_row(a, row, given, zt, poison ? NAN : m, n, s, poison ? NAN : q, lt);
+            log_s = lt;
+        }
     }
     if (a.k == 0) return;
 
@@ -449,6 +452,7 @@ __global__ __launch_bounds__(PT) void score_kernel(const ScoreArgs a)
         got = have < a.k ? have : a.k;
     }
     // a key's place is the number of larger ones, counted by eight lanes; places beyond the last key hold nothing
+    const float lt = log_s;                            // (a barrier ago at least; segments have no use for it)
     for (int c = tid >> 3; c < got; c += T >> 3) {
         const key_t mine = cand[c];
         int place = 0;
