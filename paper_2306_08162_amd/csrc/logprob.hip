@@ -517,7 +517,7 @@ __global__ __launch_bounds__(JOIN_T) void score_join_kernel(const ScoreArgs a)
     s = wave_total(s);
     q = wave_total(q);
     const float lt = poison ? NAN : m == -INFINITY ? 0.f : log_total(n, s);
-    if (tid == 0) write_row(a, row, given, zt, poison ? NAN : m, n, s, poison ? NAN : q, lt);
+    if (tid == 0) write_row(a, row, given, zt, poison ? NAN : m, n, poison ? NAN : s, poison ? NAN : q, lt);
     if (a.k == 0) return;
     int best = 0;                                                      // keys [0, best) are the best so far, in order
     for (int at = 0; at < all; at += JOIN_T) {

@@ -229,6 +229,24 @@ def test_not_finite_rows(V):
     np.testing.assert_allclose(got[[0, 3]], want, rtol=1e-4, atol=1e-6)
 
 
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_nan_in_a_masked_stretch_of_a_long_row(dtype):
+    """A row of several segments; one of them holds masked tokens and a single NaN: all that the row writes is NaN."""
+    announce(f"token logprobs NaN among masks {dtype}")
+    V = 140000
+    z = _logits(4, 3, V, dtype)
+    z[1, :30000] = -np.inf
+    z[1, 7] = np.nan
+    c = _Call(z, [40000, 40000, 5], dtype, 3)
+    c.forward()
+    c.check()
+    stats = c.stats.cpu().numpy()
+    assert np.isnan(stats[1]).all() and np.isfinite(stats[[0, 2]]).all()
+    c.backward([1, 1, 1], None)
+    got = c.dlogits.float().cpu().numpy()
+    assert np.isnan(got[1]).all() and np.isfinite(got[[0, 2]]).all()
+
+
 def test_almost_certain_tokens_keep_their_digits():
     """log p = -s of a dominant token: relative accuracy where 1 + s would round s away."""
     announce("token logprobs almost certain")
