@@ -481,7 +481,8 @@ int qlora_grad_norm(const void *plan, const void *plan_device, float grad_scale,
  * by clip = min(1, max_grad_norm / norm), and if the norm is not finite (an overflow under loss scaling) nothing changes but
  * control->skipped and grad_norm; INFINITY checks without clipping.  max_grad_norm == 0: neither; the workspace
  * may then be NULL, clip is 1, and a gradient that is not finite makes its weight and states NaN (8-bit states: its
- * block's).  Gradients are not cleared.  QLORA_E_VALUE: a beta outside [0, 1), eps or max_grad_norm negative or NaN.
+ * block's).  Gradients are not cleared.  QLORA_E_VALUE: a beta outside [0, 1), max_grad_norm negative or NaN, eps not
+ * between 2^-126 and the largest fp32 number.
  * Calls that share a control block or a workspace and overlap in time race.  Two launches.
  */
 int qlora_adamw_step(const void *plan, const void *plan_device, qlora_optim_control_t *control, double beta1, double beta2,

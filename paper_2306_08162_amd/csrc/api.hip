@@ -7,6 +7,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <mutex>
 #include <new>
@@ -1012,7 +1013,8 @@ int qlora_adamw_step(const void *plan, const void *plan_device, qlora_optim_cont
     if (st != QLORA_OK) return st;
     if (!h.steppable) return QLORA_E_PLAN;
     if (!control) return QLORA_E_NULL;
-    if (!beta_ok(beta1) || !beta_ok(beta2) || !(eps >= 0.0 && eps < INFINITY) || !(max_grad_norm >= 0.0)) return QLORA_E_VALUE;
+    // (below the smallest normal number the division would make NaN of a weight that has not seen a gradient)
+    if (!beta_ok(beta1) || !beta_ok(beta2) || !(eps >= FLT_MIN && eps <= FLT_MAX) || !(max_grad_norm >= 0.0)) return QLORA_E_VALUE;
     if (misaligned(control) || misaligned(workspace)) return QLORA_E_ALIGN;
     if (max_grad_norm > 0.0 && (!workspace || workspace_bytes < qlora_optim_workspace_bytes())) return QLORA_E_WORKSPACE;
     begin_call();

@@ -304,6 +304,19 @@ def test_norm(grad, size):
     assert np.isnan(float(out))
 
 
+@pytest.mark.parametrize("bits", [8, 32])
+def test_smallest_eps_without_a_gradient(bits):
+    announce(f"adamw eps 2^-126 bits={bits}")
+    s = _Set(34, param="f32", bits=bits)
+    for i in range(len(s.sizes)):
+        s.put("grad", i, np.zeros(s.sizes[i]))
+    before = [s.get("param", i) for i in range(len(s.sizes))]
+    s.optimizer(lr=1.0, eps=2.0 ** -126).step()
+    for i, w in enumerate(before):
+        ratio, wd = s.hyper(i)
+        assert np.all(np.abs(s.get("param", i) - w * (1 - ratio * wd)) <= 3 * U * np.abs(w))
+
+
 def test_no_gradient_at_all():
     announce("adamw zero gradients, clipped")
     s = _Set(33, param="f32")

@@ -128,6 +128,13 @@ def test_step_refusals(change, status):
                                a["wsb"], stream=0, check=False) == E["QLORA_E_" + status]
 
 
+@pytest.mark.parametrize("eps", [0.0, 1e-45, 2.0 ** -127, 1e39, float("nan")])
+def test_step_refuses_an_eps_that_fp32_does_not_hold(eps):
+    """With none (or one that the division flushes) a weight without a gradient, as A's are while B is 0, would become NaN."""
+    plan = ql.qlora_optim_plan([_tensor()])
+    assert ql.qlora_adamw_step(plan, FAKE, FAKE, 0.9, 0.999, eps, 0.0, None, stream=0, check=False) == E["QLORA_E_VALUE"]
+
+
 def test_step_refuses_other_plans():
     step = lambda plan: ql.qlora_adamw_step(plan, FAKE, FAKE, 0.9, 0.999, 1e-8, 0.0, None, stream=0, check=False)
     assert step(ctypes.create_string_buffer(4096)) == E["QLORA_E_PLAN"]
