@@ -456,7 +456,7 @@ typedef struct {
     float lr, grad_scale;           /* the caller's: read by every step */
     uint32_t seed;                  /* the caller's: 8-bit states */
     int32_t step;                   /* steps taken */
-    int32_t skipped;                /* calls that took none because the gradients were not finite */
+    int32_t skipped;                /* calls that took none because the gradients were not finite (or too large) */
     float grad_norm;                /* of the last call that looked, times grad_scale, before clipping */
     float rate, root;               /* of the step under way: lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t) */
     double beta1_power, beta2_power;        /* beta^step */
@@ -478,10 +478,11 @@ int qlora_grad_norm(const void *plan, const void *plan_device, float grad_scale,
 
 /*
  * One step.  max_grad_norm > 0: the norm is taken first, control->grad_norm receives it, the gradients are scaled
- * by clip = min(1, max_grad_norm / norm), and if the norm is not finite (an overflow under loss scaling) nothing changes but
- * control->skipped and grad_norm; INFINITY checks without clipping.  max_grad_norm == 0: neither; the workspace
+ * by clip = min(1, max_grad_norm / norm), and if the norm is not finite (an overflow under loss scaling), or not below 2^63
+ * after clipping (exp_avg_sq would overflow), nothing changes but control->skipped and grad_norm; INFINITY checks without
+ * clipping.  max_grad_norm == 0: neither; the workspace
  * may then be NULL, clip is 1, and a gradient that is not finite makes its weight and states NaN (8-bit states: its
- * block's).  Gradients are not cleared.  QLORA_E_VALUE: a beta outside [0, 1), max_grad_norm negative or NaN, eps not
+ * block's); one above 1.8e19, whose square is not finite, overflows exp_avg_sq.  Gradients are not cleared.  QLORA_E_VALUE: a beta outside [0, 1), max_grad_norm negative or NaN, eps not
  * between 2^-126 and the largest fp32 number.
  * Calls that share a control block or a workspace and overlap in time race.  Two launches.
  */

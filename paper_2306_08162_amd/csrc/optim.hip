@@ -381,7 +381,8 @@ __device__ __forceinline__ void step_chunk(const AdamArgs &a, const OptimChunk &
         __shared__ float clipped;                                      // NaN: the step is not taken
         if (wave == 0) {
             const double norm = sqrt(sum_parts(parts)) * fabs((double)gscale), clip = a.max_norm / norm;
-            const bool finite = (float)norm < INFINITY;
+            // what is left of a gradient after clipping is at most min(norm, max_norm): its square has to stay in fp32
+            const bool finite = (float)norm < INFINITY && (norm < 0x1p63 || a.max_norm < 0x1p63);
             if (lane == 0) clipped = finite ? gscale * (float)(clip < 1.0 ? clip : 1.0) : NAN;     // (norm 0: nothing to clip)
             if (blockIdx.x == 0 && lane == 0) {
                 a.control->grad_norm = (float)norm;

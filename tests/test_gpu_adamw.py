@@ -233,7 +233,9 @@ def test_zero_and_tiny_second_moments():
     assert (codes[256:512] > 0).all()
     w = s.get("param", 0)
     assert (w[:256] == 0).all() and np.isfinite(w).all()
-    # |m| <= 0.1 and sqrt v >= 2^-9 of the scale, which is 2^-13 for a largest sqrt v of 0.0316: bounded by the codes
+    # Of exact moments |m| / sqrt v <= (1 - b1) / sqrt((1 - b2) (1 - b1^2 / b2)) = 7.28, and the bias corrections,
+    # sqrt(1 - b2^t) / (1 - b1^t) <= 0.32 (t = 1), leave less of it.  Of the tiny weights both codes are at most the lowest but
+    # one here: m <= 2^-9 of a scale of 2^-12, sqrt v >= 2^-9 of 2^-13, a ratio of 2.  30 steps of at most 7.3 are more than either.
     assert np.abs(w).max() < 30 * 7.3
 
 
@@ -266,6 +268,27 @@ def test_steps_on_gradients_that_overflowed_are_not_taken(bits, bad):
     for n, b in s.buf.items():
         assert torch.equal(b, once[n]), n
     assert int(opt.steps_taken) == 2
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_gradients_whose_squares_leave_fp32(bits):
+    """A gradient of 1e20: without clipping the step is not taken, clipped to a norm of 1 it is."""
+    import torch
+    announce(f"adamw large gradients bits={bits}")
+    s = _Set(23, sizes=(600, 300), param="f32", bits=bits)
+    s.view("grad", 0)[300] = 1e20
+    kept = {n: b.clone() for n, b in s.buf.items()}
+    opt = s.optimizer(lr=1e-2, max_grad_norm=np.inf)
+    opt.step()
+    assert (int(opt.steps_taken), int(opt.steps_skipped)) == (0, 1) and abs(float(opt.last_grad_norm) / 1e20 - 1) < 1e-6
+    assert all(torch.equal(b, kept[n]) for n, b in s.buf.items())
+    opt = s.optimizer(lr=1e-2, max_grad_norm=1.0)
+    opt.step()
+    assert (int(opt.steps_taken), int(opt.steps_skipped)) == (1, 0)
+    for n in ("param", "exp_avg_sq"):
+        assert all(np.isfinite(s.get(n, i)).all() for i in range(2)), n
+    # g = 1: the first step is lr (1 - b) / sqrt(1 - b2) / (its bias correction) = lr, after the weight's own decay (0.0)
+    assert abs(s.get("param", 0)[300] - (kept["param"][s.at[0] + 300].item() - 1e-2)) <= 64 * U
 
 
 def test_unguarded_steps_keep_the_damage_where_it_is():
