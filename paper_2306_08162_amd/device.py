@@ -357,9 +357,17 @@ class AdapterOptimizer:
         self.device_grad_scale = words[1:2]
         counts = self.control.view(torch.int32)
         self.steps_taken, self.steps_skipped = counts[3:4], counts[4:5]
+        if self.device.type == "cuda":                                      # steps may follow on any stream
+            torch.cuda.current_stream(self.device).synchronize()
 
     def _upload(self, host) -> torch.Tensor:
         return torch.frombuffer(bytearray(host), dtype=torch.uint8).to(self.device)
+
+    @staticmethod
+    def _flag(b: torch.Tensor, name: str) -> int:
+        if b.dtype not in _FLAG:
+            raise ValueError(f"{name} of {b.dtype}: {name}_dtype has to say what it holds")
+        return _FLAG[b.dtype]
 
     def _describe(self, t: OptimTensor) -> ql.OptimTensorStruct:
         n, s = t.grad.numel(), ql.OptimTensorStruct()
@@ -383,11 +391,11 @@ class AdapterOptimizer:
                     continue
                 if b.numel() != size or (bytes_each and b.element_size() != bytes_each):
                     raise ValueError(f"{name} of {b.numel()} x {b.element_size()} bytes beside a gradient of {n} entries")
-            s.param_dtype = _FLAG[t.param.dtype] if t.param_dtype is None else t.param_dtype
+            s.param_dtype = self._flag(t.param, "param") if t.param_dtype is None else t.param_dtype
             if t.param.element_size() != (4 if s.param_dtype == ql.QLORA_F32 else 2):
                 raise ValueError("param_dtype does not fit the tensor")
             s.lr_scale, s.weight_decay, s.state_bits = t.lr_scale, t.weight_decay, t.state_bits
-        s.grad_dtype = _FLAG[t.grad.dtype] if t.grad_dtype is None else t.grad_dtype
+        s.grad_dtype = self._flag(t.grad, "grad") if t.grad_dtype is None else t.grad_dtype
         if t.grad.element_size() != (4 if s.grad_dtype == ql.QLORA_F32 else 2):
             raise ValueError("grad_dtype does not fit the tensor")
         s.numel = n
@@ -412,5 +420,7 @@ class AdapterOptimizer:
     def grad_norm(self, out: torch.Tensor, grad_scale: Optional[float] = None, stream=None) -> None:
         """out [1] fp32: the norm of all gradients, times the grad_scale the optimizer was made with (or this one)."""
         self._here()
+        if out.dtype != torch.float32 or out.numel() < 1 or out.device != self.device:
+            raise ValueError("the norm is written into an fp32 tensor on the gradients' device")
         ql.qlora_grad_norm(self.plan, self._plan_ptr, self.grad_scale if grad_scale is None else grad_scale, out,
                            self._workspace_ptr, self._workspace_bytes, stream=stream)

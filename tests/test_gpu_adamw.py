@@ -427,6 +427,37 @@ def test_step_on_another_stream_and_refused_tensors():
         AdapterOptimizer([OptimTensor(w, t(64)), OptimTensor(w, t(64))], lr=1e-3)
 
 
+def test_states_it_allocates_are_ready_on_any_stream():
+    """400 MB of states are cleared on the current stream; a step on another one right after finds zeros."""
+    import torch
+    from paper_2306_08162_amd.device import AdapterOptimizer, OptimTensor
+    announce("adamw own states, other stream")
+    n = 50_000_000
+    dirty = [torch.full((n,), float("nan"), device="cuda:0") for _ in range(2)]   # what the allocator hands out again
+    torch.cuda.synchronize()
+    w, g, side = torch.zeros(n, device="cuda:0"), torch.ones(n, device="cuda:0"), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    del dirty
+    AdapterOptimizer([OptimTensor(w, g)], lr=0.5).step(stream=side)
+    side.synchronize()
+    # the first step is lr g / (|g| + eps): within the dozen roundings and two approximations of 32 u
+    assert float((w + 0.5).abs().max()) <= 0.5 * 32 * U + 1e-8
+
+
+def test_tensors_of_unknown_contents_and_norms_elsewhere_are_refused():
+    import torch
+    from paper_2306_08162_amd.device import AdapterOptimizer, OptimTensor
+    announce("adamw refusals of types")
+    t = lambda n, dtype=torch.float32: torch.zeros(n, dtype=dtype, device="cuda:0")
+    for bad in (OptimTensor(t(8, torch.int16), t(8)), OptimTensor(t(8), t(8, torch.float64))):
+        with pytest.raises(ValueError):
+            AdapterOptimizer([bad], lr=1e-3)
+    opt = AdapterOptimizer([OptimTensor(t(8), t(8))], lr=1e-3)
+    for out in (t(1, torch.float64), t(0), t(1).cpu()):
+        with pytest.raises(ValueError):
+            opt.grad_norm(out)
+
+
 def test_adapters_learn_from_token_scores():
     """The calls of a training step in a row: a quantized head with adapters makes logits, the tokens are scored, the gradient
     of their log probabilities goes back through the layer into dA and dB, and the optimizer moves A and B; every
