@@ -394,6 +394,75 @@ def test_graph_replays_match_eager():
             assert torch.equal(a, b), f"replay {rep}"
 
 
+@pytest.mark.parametrize("kind", ["normal", "rising", "constant"])
+@pytest.mark.parametrize("M,dtype", [(1, "f32"), (2, "f16")])
+def test_rows_of_many_segments(M, dtype, kind):
+    """1.5 million tokens: more segments than a wave has lanes, and lists of 64 alternatives of each to be joined."""
+    announce(f"token logprobs {M} x 1500001 {dtype} {kind}")
+    V = 1500001
+    i = np.arange(V)
+    z = {"normal": lambda: _logits(9, M, V, dtype), "rising": lambda: np.tile(_rounded(i / 2.0 ** 17, dtype), (M, 1)),
+         "constant": lambda: np.full((M, V), -2.5)}[kind]()
+    c = _Call(z, np.array([V - 1, 7])[:M], dtype, 64)
+    c.forward()
+    c.check()
+    c.backward(np.ones(M), np.ones(M))
+    c.check_gradient()
+
+
+def test_longest_row():
+    """2^28 tokens.  All logits are 0 but 20 in places from the first to the last; the sums are then known."""
+    import torch
+    announce("token logprobs 1 x 2^28 f16")
+    V, k = 1 << 28, 21
+    z = torch.zeros((1, V), dtype=torch.float16, device="cuda:0")
+    at = [int(p) for p in np.linspace(0, V - 1, 20)]
+    high = 12.0 + np.arange(20) / 4.0
+    z[0, torch.tensor(at, device="cuda:0")] = torch.from_numpy(high).half().cuda()
+    dev = lambda shape, t=torch.float32: torch.full(shape, 9, dtype=t, device="cuda:0")
+    lp, H, st, alt, alp, token = dev((1,)), dev((1,)), dev((1, 4)), dev((1, k), torch.int32), dev((1, k)), dev((1,), torch.int32)
+    token.fill_(V - 1)
+    ws = torch.empty(ql.qlora_token_logprobs_workspace_bytes(1, V, k, ql.QLORA_F16), dtype=torch.uint8, device="cuda:0")
+    ql.qlora_token_logprobs(z, V, token, lp, H, alt, alp, k, st, 1, V, ql.QLORA_F16, ws)
+    total = np.exp(high).sum() + (V - 20)
+    want = np.concatenate([high[::-1], [0.0]]) - np.log(total)
+    entropy = np.log(total) - (np.exp(high) * high).sum() / total
+    ls = np.log(total) - high[-1]
+    assert alt[0].tolist() == at[::-1] + [1]
+    # a lane adds up to 64 equal weights, 2^12 segments are joined by 64 additions a lane: the module's C covers both
+    assert np.all(np.abs(alp[0].cpu().numpy() - want) <= C * U * (1 + np.abs(want) + ls))
+    assert abs(float(lp) - want[0]) <= C * U * (1 + abs(want[0]) + ls)
+    assert abs(float(H) - entropy) <= C * U * (1 + entropy + ls)
+    g = torch.ones(1, device="cuda:0")
+    ql.qlora_token_logprobs_bwd(z, V, token, st, g, None, z, V, 1, V, ql.QLORA_F16)
+    p = np.exp(want)
+    got = z[0, torch.tensor(at[::-1], device="cuda:0")].double().cpu().numpy()
+    exact = np.eye(20)[0] - p[:20]
+    off = C * U * p[:20] * (1 + np.abs(want[:20]) + ls)
+    assert np.all(np.abs(got - exact) <= off + HALF_ULP["f16"] * 1.01 * np.abs(exact) + TINY["f16"] * 1.01)
+    rest = z[0].count_nonzero().item()                      # the others' -p = 1 / total is below fp16's smallest number
+    assert rest == 20 and p[20] < TINY["f16"]
+
+
+def test_two_calls_at_once():
+    """Two streams, each with its own workspace and outputs, find what one does."""
+    import torch
+    announce("token logprobs two streams")
+    calls = [_Call(_logits(40 + i, 12, 90001, "f16"), _tokens(40 + i, 12, 90001), "f16", 20) for i in range(2)]
+    outs = lambda c: [t.clone() for t in (c.logprob, c.entropy, c.alt, c.alt_lp, c.stats)]
+    for c in calls:
+        c.forward()
+    first = [outs(c) for c in calls]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(20):
+        for c, s in zip(calls, streams):
+            c.forward(stream=s)
+    torch.cuda.synchronize()
+    for c, was in zip(calls, first):
+        assert all(torch.equal(a, b) for a, b in zip(was, outs(c)))
+
+
 def test_logits_beyond_four_gigabytes():
     """Offsets that pass 32 bits, of elements and of bytes: sampled rows of 70000 x 32000, scored and differentiated in place."""
     import torch
