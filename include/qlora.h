@@ -460,7 +460,7 @@ typedef struct {
     float grad_norm;                /* of the last call that looked, times grad_scale, before clipping */
     float rate, root;               /* of the step under way: lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t) */
     double beta1_power, beta2_power;        /* beta^step */
-    uint32_t key, reserved[3];
+    uint32_t key, arrived, reserved[2];     /* arrived: 0 between calls */
 } qlora_optim_control_t;
 /* HOST memory: a control block after `step` steps (0: a fresh start).  QLORA_E_VALUE: a beta outside [0, 1), step < 0. */
 int qlora_optim_control_init(qlora_optim_control_t *control, float lr, float grad_scale, uint32_t seed, int32_t step,
@@ -484,7 +484,8 @@ int qlora_grad_norm(const void *plan, const void *plan_device, float grad_scale,
  * may then be NULL, clip is 1, and a gradient that is not finite makes its weight and states NaN (8-bit states: its
  * block's); one above 1.8e19, whose square is not finite, overflows exp_avg_sq.  Gradients are not cleared.  QLORA_E_VALUE: a beta outside [0, 1), max_grad_norm negative or NaN, eps not
  * between 2^-126 and the largest fp32 number.
- * Calls that share a control block or a workspace and overlap in time race.  Two launches.
+ * Calls that share a control block or a workspace and overlap in time race.  Two launches;
+ * one where max_grad_norm is 0 and the plan small.
  */
 int qlora_adamw_step(const void *plan, const void *plan_device, qlora_optim_control_t *control, double beta1, double beta2,
                      double eps, double max_grad_norm, void *workspace, size_t workspace_bytes, void *stream);

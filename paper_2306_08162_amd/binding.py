@@ -54,7 +54,7 @@ class OptimControlStruct(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_float), ("grad_scale", ctypes.c_float), ("seed", ctypes.c_uint32),
                 ("step", ctypes.c_int32), ("skipped", ctypes.c_int32), ("grad_norm", ctypes.c_float),
                 ("rate", ctypes.c_float), ("root", ctypes.c_float), ("beta1_power", ctypes.c_double),
-                ("beta2_power", ctypes.c_double), ("key", ctypes.c_uint32), ("reserved", ctypes.c_uint32 * 3)]
+                ("beta2_power", ctypes.c_double), ("key", ctypes.c_uint32), ("arrived", ctypes.c_uint32), ("reserved", ctypes.c_uint32 * 2)]
 
 
 class QLoraError(RuntimeError):

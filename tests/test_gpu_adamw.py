@@ -400,6 +400,54 @@ def test_graph_replays_match_eager(bits):
     assert int(b.steps_taken) == 5 and int(b.steps_skipped) == 1
 
 
+@pytest.mark.parametrize("bits", [8, 32])
+def test_small_and_large_plans_take_the_same_step(bits):
+    """Without clipping: 128 chunks of a plan are one launch, 129 are two; the tensors of both and the control block agree."""
+    import torch
+    announce(f"adamw 128 and 129 chunks bits={bits}")
+    sizes = (2048 * 120 + 7, 300, 2048 * 5 + 1)
+    one, two = _Set(71, sizes=sizes, param="bf16", bits=bits), _Set(71, sizes=sizes + (5,), param="bf16", bits=bits)
+    kw = dict(lr=1e-2, betas=(0.9, 0.99), seed=5)
+    a, b = one.optimizer(**kw), two.optimizer(**kw)
+    assert [ql.qlora_optim_plan_bytes([o._describe(t) for t in o.tensors]) for o in (a, b)] == [64 + 80 * 128, 64 + 80 * 129]
+    for t in range(5):
+        for s, o in ((one, a), (two, b)):
+            s.gradient(t)
+            o.step()
+        assert torch.equal(a.control, b.control), t
+        for n in one.buf:
+            for i in range(len(sizes)):
+                assert torch.equal(one.view(n, i), two.view(n, i)), (t, n, i)
+    assert int(a.steps_taken) == 5
+    one.untouched_between()
+    two.untouched_between()
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_graph_replays_of_a_small_step_match_eager(bits):
+    import torch
+    announce(f"adamw graph of one launch bits={bits}")
+    eager, captured = (_Set(52, bits=bits, param="f16") for _ in range(2))
+    a, b = eager.optimizer(lr=1e-2, seed=6), captured.optimizer(lr=1e-2, seed=6)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        b.step()
+        b.step()
+    for t in range(6):
+        for s, o in ((eager, a), (captured, b)):
+            s.gradient(t)
+            o.lr.fill_(1e-2 / (t + 1))
+        a.step()
+        a.step()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(a.control, b.control), t
+        for n in eager.buf:
+            assert torch.equal(eager.buf[n], captured.buf[n]), (t, n)
+    assert int(b.steps_taken) == 12
+
+
 def test_step_on_another_stream_and_refused_tensors():
     import torch
     from paper_2306_08162_amd.device import AdapterOptimizer, OptimTensor
