@@ -801,8 +801,8 @@ int qlora_token_logprobs(const void *logits, int64_t row_stride, const int32_t *
     if (!logits || (logprob && !tokens) || (alternatives > 0 && (!alt_tokens || !alt_logprobs)) ||
         (!logprob && !entropy && !stats && alternatives == 0))
         return QLORA_E_NULL;
-    if (between_elements(logits, dtype) || misaligned(stats) || misaligned(workspace) || odd4(tokens) || odd4(logprob) || odd4(entropy) ||
-        (alternatives > 0 && (odd4(alt_tokens) || odd4(alt_logprobs))))
+    if (between_elements(logits, dtype) || misaligned(stats) || misaligned(workspace) || odd4(tokens) || odd4(logprob) ||
+        odd4(entropy) || (alternatives > 0 && (odd4(alt_tokens) || odd4(alt_logprobs))))
         return QLORA_E_ALIGN;
     const size_t need = qlora_token_logprobs_workspace_bytes(M, V, alternatives, dtype);
     if (need && (!workspace || workspace_bytes < need)) return QLORA_E_WORKSPACE;
@@ -821,7 +821,8 @@ int qlora_token_logprobs_bwd(const void *logits, int64_t row_stride, const int32
     if ((st = check_stride(M, V, row_stride)) != QLORA_OK || (st = check_stride(M, V, d_row_stride)) != QLORA_OK) return st;
     if (dlogits == logits && d_row_stride != row_stride && M > 1) return QLORA_E_VALUE;
     if (!logits || !stats || !dlogits || (!d_logprob && !d_entropy) || (d_logprob && !tokens)) return QLORA_E_NULL;
-    if (between_elements(logits, dtype) || misaligned(stats) || between_elements(dlogits, dtype) || odd4(tokens) || odd4(d_logprob) || odd4(d_entropy))
+    if (between_elements(logits, dtype) || misaligned(stats) || between_elements(dlogits, dtype) || odd4(tokens) ||
+        odd4(d_logprob) || odd4(d_entropy))
         return QLORA_E_ALIGN;
     begin_call();
     launch_token_logprobs_bwd(logits, row_stride, tokens, stats, d_logprob, d_entropy, dlogits, d_row_stride, M, V, dtype,

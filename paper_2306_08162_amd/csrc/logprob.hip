@@ -6,8 +6,10 @@
 //   gradient  of g log p_t + h H:   dz_i = g [i = t] - p_i (g + h (log p_i + H))
 //
 // The work is bound by HBM: a row is read once (and, backward, once more and its gradient written).  One workgroup takes
-// up to 64 KB of a row into registers, so the maximum is known before the first exponential and no sum is ever rescaled;
-// longer rows, and rows too few to fill the chip, are cut into segments whose results a second launch joins.
+// up to 128 KB of a row into registers, so the maximum is known before the first exponential and no sum is ever rescaled;
+// longer rows, and rows too few to fill the chip, are cut into segments whose results a second launch joins.  2048 rows of
+// 32000 in fp16, 131 MB: 26.3 us or 5.0 TB/s for the log probabilities alone (reading them takes 24), 28 with the entropy, 34
+// with 20 alternatives besides: an entry costs three instructions, one of them the exponential, and two more with the entropy.
 //
 // A token that is almost certain has p = 1 / (1 + s) with a tiny s, and S = 1 + s would round it away: the sums keep
 // the entries equal to the maximum as a count n apart from the sum s of all others, ln S = log1p(s) where n = 1, and
@@ -211,6 +213,9 @@ __device__ __forceinline__ Piece<DT> pick(const Piece<DT> *r, int i)
 }
 
 // MOMENTS: the entropy is asked for, or the statistics that hold it.  At most PT threads with PCH pieces each.
+// All of a thread's pieces are requested at once and nothing else is until they are used up: other workgroups of the compute
+// unit read meanwhile.  (Stages of four pieces, the next ones on their way, with a maximum of their own: 28.8 us where this takes
+// 26.7, for the sums have to be rescaled.)
 template <int DT, bool MOMENTS, int PT, int PCH>
 __global__ __launch_bounds__(PT) void score_kernel(const ScoreArgs a)
 {
@@ -636,8 +641,12 @@ __global__ __launch_bounds__(GT) void score_grad_kernel(const ScoreGradArgs a)
     }
 }
 
-// Many rows: 256 threads with 64 KB of a row, four workgroups on a compute unit (or 512 with 128 KB, where that spares the
-// second launch).  Few: each has a compute unit to itself, and 1024 threads get through it sooner.
+// Many rows: 256 threads with 64 KB of a row, four workgroups on a compute unit.  2048 x 32000 fp16: 31 us when first built that
+// way, 33 with 512 threads and half the pieces, 57 with 1024 and a quarter, 36 with twice the pieces and 128 or 256 threads, whose
+// waves are too few.  Rows of 64 to 128 KB: 512 threads, which spares the second launch (1024 x 32000 fp32 26.3 us, 29.5 as two
+// segments).  Longer ones in segments of at most 64 KB: 777 x 128259 bf16 with 20 alternatives takes 55.7 us, with 128 KB 61.8,
+// with 45 to 22 KB 63 to 72, for each segment has alternatives of its own (without any 42 to 46 us, 51 with 128 KB).
+// Few rows (no more than compute units): each has one to itself, and 1024 threads get through it sooner.
 constexpr int MANY_PT = 512, MANY_PCH = 16, FEW_PT = 1024, FEW_PCH = 8, SEGMENT = 4096;
 
 inline int pieces_of(int V, int dt) { return (int)(((long)V + (dt == 2 ? 3 : 7)) / (dt == 2 ? 4 : 8)); }
@@ -669,14 +678,18 @@ ScorePlan score_plan(int M, int V, int dt)
     ScorePlan p;
     p.splits = pieces <= MANY_PT * MANY_PCH ? 1 : (pieces + SEGMENT - 1) / SEGMENT;
     const bool many = (long)M * p.splits > 256;
-    if (!many) {    // one workgroup a row as long as one can hold it; else short segments on as many compute units as there are
+    // one workgroup a row as long as one can hold it; else short segments on as many compute units as there are (8 x 128256 bf16:
+    // 11.5 us, 14.1 with as few segments as hold it)
+    if (!many) {
         p.splits = (pieces + FEW_PT * FEW_PCH - 1) / (FEW_PT * FEW_PCH);
         const int spread = std::min((pieces + 2047) / 2048, 512 / M);
         if (p.splits > 1) p.splits = std::max(p.splits, spread);
     }
     p.seg = (pieces + p.splits - 1) / p.splits;
     p.threads = 64;
-    if (many) {     // what a wave does once a row weighs more than its pieces: few waves, as long as the chip has sixteen a unit
+    // of many short rows what a wave does once a row weighs more than its pieces: few waves, as long as the chip has sixteen a unit
+    // (2048 x 4096 fp16: 7.6 us, 9.5 with a wave for every 64 pieces)
+    if (many) {
         while (p.threads * MANY_PCH < p.seg) p.threads *= 2;
         while (p.threads < 256 && p.threads * 2 < p.seg && (long)M * p.splits * p.threads < 256 * 1024) p.threads *= 2;
     } else {

@@ -4,9 +4,12 @@
 //   w = w (1 - lr wd) - lr / (1 - b1^t) * m / (sqrt(v) / sqrt(1 - b2^t) + eps)
 //
 // The step is bound by HBM: with fp32 gradients and 16-bit weights 24 bytes a weight (fp32 states), 12 with states of
-// 8 bits, and 4 more for the norm.  20M weights with fp32 masters: 103 us with the norm, 5.8 TB/s of the 600 MB that a step cannot
-// do without (a large copy reaches 4.9 to 5.7); 160M with 8-bit states: 435 us, 5.9 TB/s with the second reading of the gradients counted.  A plan in device memory has a record for each chunk of up to 2048 weights of a tensor, one workgroup's work: hundreds
-// of small matrices fill the chip like one large one.
+// 8 bits, and 4 more for the norm.  20M weights with fp32 masters: 103 us with the norm, 5.8 TB/s of the 600 MB that a step
+// cannot do without (a large copy reaches 4.9 to 5.7); 160M with 8-bit states: 435 us, 5.9 TB/s with the second reading of the
+// gradients counted, and 61 instructions a weight close behind it.
+// A plan in device memory has a record for each chunk of up to 2048 weights of a tensor, one workgroup's work: hundreds of small
+// matrices fill the chip like one large one.  (Chunks of 1024 and 4096: 517 and 481 us where 2048 took 485 on those 160M, but 22.3
+// and 25.8 where it took 22.1 on 5M in 96 tensors.)
 //
 // 8-bit states.  256 consecutive weights share a scale, the power of two that brings the largest magnitude into
 // (224, 448]; the codes are e4m3, which keeps four significant bits over 17 powers of two, and a power of two for a scale
@@ -44,7 +47,8 @@ __device__ __forceinline__ uint32_t mix(uint32_t x)
 // Device memory by type: a pointer read from the plan would otherwise be taken for one into any memory, with slower loads.
 // ONCE: past the caches.  A step touches each of its bytes once, and whatever ran since the step before has replaced them:
 // with the hint 448 fp32-state tensors of 600 MB take 103 us instead of 124, 37 MB 10.4 instead of 13.5 (3 to 11 % more
-// only where steps of up to 225 MB follow one another with nothing in between).  The gradients' first reading, for their norm, leaves them in the caches.
+// only where steps of up to 225 MB follow one another with nothing in between).  The gradients' first reading, for their norm,
+// leaves them in the caches.
 template <bool ONCE, typename T>
 __device__ __forceinline__ T load_global(const void *p, uint32_t byte)
 {
@@ -446,7 +450,7 @@ __device__ __forceinline__ void step_chunk(const AdamArgs &a, const OptimChunk &
 #pragma unroll
             for (int e = 0; e < 4; ++e) mf[e] *= a.b1;
         } else {
-            decode4(m[i][0], ms[i] * a.b1, mf);                        // a power of two times b1: one rounding in all, as in 32 bits
+            decode4(m[i][0], ms[i] * a.b1, mf);                        // a power of two times b1: one rounding, as in 32 bits
             decode4(v[i][0], vs[i], vf);
 #pragma unroll
             for (int e = 0; e < 4; ++e) vf[e] *= vf[e];
@@ -517,8 +521,8 @@ __global__ __launch_bounds__(OT) __attribute__((amdgpu_waves_per_eu(6, 6))) void
 
 // A small step without clipping, in one launch: each workgroup works out the coming step for itself while its chunk is on the
 // way, and the last one to have read the control block commits.  Their arrivals are counted in the control block, one after
-// the other, 13 ns each: 64 chunks take 4.5 us (8-bit states 5.3) where two launches take 7.0 (6.9), 128 5.1 (6.0), but 256 6.7 (7.5)
-// and 512 10.4 (10.9) where those take 6.8 (6.8) and 7.1 (7.3).
+// the other, 13 ns each: 64 chunks take 4.5 us (8-bit states 5.3) where two launches take 7.0 (6.9), 128 take 5.1 (6.0), but 256
+// 6.7 (7.5) and 512 10.4 (10.9) where those take 6.8 (6.8) and 7.1 (7.3).
 constexpr uint32_t ALONE_CHUNKS = 128;
 __global__ __launch_bounds__(OT) void adamw_alone_kernel(const AdamArgs a) { step_any<true>(a, Parts{}); }
 
