@@ -349,7 +349,7 @@ class AdapterOptimizer:
         control = ql.qlora_optim_control_init(lr, grad_scale, seed, step, *self.betas)
         self.control = self._upload(control)
         self.workspace = torch.empty(ql.qlora_optim_workspace_bytes(), dtype=torch.uint8, device=self.device)
-        # taken once: a step's host time is that of its two launches
+        # taken once: a step's host time is that of its launches
         self._plan_ptr, self._control_ptr = self.plan_device.data_ptr(), self.control.data_ptr()
         self._workspace_ptr, self._workspace_bytes = self.workspace.data_ptr(), self.workspace.numel()
         words = self.control.view(torch.float32)
