@@ -343,6 +343,8 @@ class AdapterOptimizer:
         if not self.tensors:
             raise ValueError("no tensors")
         self.device = self.tensors[0].grad.device
+        if self.device.type != "cuda":
+            raise ValueError(f"the tensors of a step live on a GPU, not on {self.device}")
         self.betas, self.eps, self.max_grad_norm, self.grad_scale = tuple(betas), eps, max_grad_norm, grad_scale
         self.plan = ql.qlora_optim_plan([self._describe(t) for t in self.tensors])
         self.plan_device = self._upload(self.plan)
@@ -357,8 +359,7 @@ class AdapterOptimizer:
         self.device_grad_scale = words[1:2]
         counts = self.control.view(torch.int32)
         self.steps_taken, self.steps_skipped = counts[3:4], counts[4:5]
-        if self.device.type == "cuda":                                      # steps may follow on any stream
-            torch.cuda.current_stream(self.device).synchronize()
+        torch.cuda.current_stream(self.device).synchronize()                # steps may follow on any stream
 
     def _upload(self, host) -> torch.Tensor:
         return torch.frombuffer(bytearray(host), dtype=torch.uint8).to(self.device)
@@ -409,7 +410,7 @@ class AdapterOptimizer:
         return s
 
     def _here(self):
-        if self.device.type == "cuda" and torch.cuda.current_device() != self.device.index:
+        if torch.cuda.current_device() != self.device.index:
             raise ValueError(f"the tensors live on {self.device}, which is not the current device")
 
     def step(self, stream=None) -> None:

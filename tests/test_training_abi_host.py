@@ -160,3 +160,10 @@ def test_control_block():
 def test_new_status_strings():
     texts = [ql.status_string(i) for i in range(len(ql.STATUS_NAMES))]
     assert len(set(texts)) == len(texts) and "unknown status" not in texts
+
+
+def test_optimizer_refuses_tensors_in_host_memory():
+    import torch
+    from paper_2306_08162_amd.device import AdapterOptimizer, OptimTensor
+    with pytest.raises(ValueError):
+        AdapterOptimizer([OptimTensor(torch.zeros(8), torch.zeros(8))], lr=1e-3)
