@@ -360,16 +360,18 @@ __global__ __launch_bounds__(PT) void score_kernel(const ScoreArgs a)
     n = wave_total(lane < waves ? red[2][lane] : 0.f);
     s = wave_total(lane < waves ? red[3][lane] : 0.f);
     if constexpr (MOMENTS) q = wave_total(lane < waves ? red[4][lane] : 0.f);
-    // w = 2^(x - slip): q = sum of w (x - slip)
-    q = (q - slip * s) * exp2_hw(-slip);
-    s *= exp2_hw(-slip);
+    // w = 2^(x - slip): q = sum of w (x - slip).  A slip below -126 belongs to a maximum past 2^30, every other entry 128 or more
+    // beneath it: s and q are exact zeros, and stay so by a factor that is finite (a NaN in s stays one by any).
+    const float back = exp2_hw(fminf(-slip, 126.f));
+    q = (q - slip * s) * back;
+    s *= back;
     const bool poison = !(s < INFINITY) || m == INFINITY;
     if (a.splits > 1) {
         if (tid == 0) a.part[(long)row * a.splits + split] = float4_t{m, n, poison ? NAN : s, q};
     } else if (last_wave) {                            // the logarithm: a hundred instructions that one wave is enough for
         const float lt = poison ? NAN : m == -INFINITY ? 0.f : log_total(n, s);
         if (lane == 0) {
-            write_row(a, row, given, zt, poison ? NAN : m, n, s, poison ? NAN : q, lt);
+            write_row(a, row, given, zt, poison ? NAN : m, n, poison ? NAN : s, poison ? NAN : q, lt);
             log_s = lt;
         }
     }

@@ -488,3 +488,66 @@ def test_logits_beyond_four_gigabytes():
     np.testing.assert_array_equal(alt[at].cpu().numpy(), walt)
     dz = scoring.score_gradient(zs, ts, np.ones(len(rows)), None)
     np.testing.assert_allclose(z[at].double().cpu().numpy(), dz, rtol=2 * HALF_ULP["f16"], atol=TINY["f16"] * 1.01)
+
+
+LARGE = (-1e10, -1e11, -1e12, -1e15, -1e18, -1e30, -1e31, -1e32)        # numbers that programs mask with
+
+
+def _check_both(z, tokens, dtype, k):
+    """Scores and gradient against the oracle; nothing of a finite row may be anything but finite."""
+    c = _Call(z, tokens, dtype, k)
+    c.forward()
+    c.check()
+    assert np.isfinite(c.logprob.cpu().numpy()).all() and np.isfinite(c.stats.cpu().numpy()).all()
+    M = len(z)
+    c.backward(np.linspace(-2, 2, M), np.linspace(1, -1, M))
+    c.check_gradient()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V,times", [(100, 1), (1000, 40), (40000, 1), (5000, 30)])
+def test_rows_of_one_large_number(V, times, dtype):
+    """Every token masked by the same finite number: a uniform distribution over all of them."""
+    announce(f"token logprobs rows of one large number V={V} {dtype}, {times} times")
+    z = _rounded(np.tile(np.repeat(np.array(LARGE)[:, None], V, axis=1), (times, 1)), dtype)
+    _check_both(z, _tokens(V, *z.shape), dtype, 5)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V,times", [(1000, 1), (33000, 1), (140003, 1), (140003, 4)])
+def test_ordinary_rows_masked_by_large_numbers(V, times, dtype):
+    """Ordinary logits beside large finite masks.  Rows of 140003 tokens are taken in segments, of which some hold the mask and nothing
+    else: at the row's head, at its tail, all but one, and all but one token."""
+    announce(f"token logprobs masked by large numbers V={V} {dtype}, {times} times")
+    rows = []
+    for i, low in enumerate(LARGE):
+        head, tail, middle, one = _logits(V + 7 * i, 4, V, dtype)
+        head[:V // 2] = low
+        tail[V - V // 3:] = low
+        middle[:V // 3], middle[V // 3 + 50:] = low, low
+        kept = one[V - 1]
+        one[:] = low
+        one[V - 1] = kept
+        rows += [head, tail, middle, one]
+    z = _rounded(np.tile(np.stack(rows), (times, 1)), dtype)
+    M = len(z)
+    tokens = np.tile([V - 1, 3, V // 3 + 7, V - 1], M // 4)
+    tokens[4::9] = 0                             # a masked target
+    _check_both(z, tokens, dtype, 20)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [900, 140003])
+def test_rows_with_a_large_maximum(V, dtype):
+    """One token far above all others, two of them at the maximum, and a neighbour one step of the type below it."""
+    import torch
+    announce(f"token logprobs large maxima V={V} {dtype}")
+    tops = _rounded(np.array([[1e9, 5e9, 1e10, 3e12, 1e20, 1e31, 3e38]]), dtype)[0]
+    M = len(tops)
+    z = np.tile(_logits(V, M, V, dtype), (3, 1))
+    for i, top in enumerate(tops):
+        below = torch.nextafter(torch.tensor(top, dtype=_torch(dtype)), torch.tensor(0.0, dtype=_torch(dtype))).item()
+        z[i, V // 2] = top
+        z[M + i, [5, V - 2]] = top
+        z[2 * M + i, [7, V - 3]] = top, below
+    _check_both(z, np.tile([V // 2, 5, V - 3], (M, 1)).T.ravel(), dtype, 3)
