@@ -335,7 +335,8 @@ class OptimTensor:
 
 class AdapterOptimizer:
     """AdamW over the adapters of a model (and whatever is trained beside them): the plan, the control block and the
-    scratch of qlora_adamw_step and qlora_grad_norm.  The tensors keep their place in memory for its lifetime."""
+    scratch of qlora_adamw_step and qlora_grad_norm.  The tensors keep their place in memory for its lifetime.  A norm
+    may be taken on another stream while a step runs; two steps, or two norms, must not overlap in time."""
 
     def __init__(self, tensors: Sequence[OptimTensor], lr: float, betas: Tuple[float, float] = (0.9, 0.999),
                  eps: float = 1e-8, max_grad_norm: float = 0.0, grad_scale: float = 1.0, seed: int = 0, step: int = 0):
@@ -350,10 +351,12 @@ class AdapterOptimizer:
         self.plan_device = self._upload(self.plan)
         control = ql.qlora_optim_control_init(lr, grad_scale, seed, step, *self.betas)
         self.control = self._upload(control)
-        self.workspace = torch.empty(ql.qlora_optim_workspace_bytes(), dtype=torch.uint8, device=self.device)
+        scratch = lambda: torch.empty(ql.qlora_optim_workspace_bytes(), dtype=torch.uint8, device=self.device)
+        self.workspace, self.norm_workspace = scratch(), scratch()
         # taken once: a step's host time is that of its launches
         self._plan_ptr, self._control_ptr = self.plan_device.data_ptr(), self.control.data_ptr()
         self._workspace_ptr, self._workspace_bytes = self.workspace.data_ptr(), self.workspace.numel()
+        self._norm_workspace_ptr = self.norm_workspace.data_ptr()
         words = self.control.view(torch.float32)
         self.lr, self.last_grad_norm = words[0:1], words[5:6]               # device floats: write lr, read the norm
         self.device_grad_scale = words[1:2]
@@ -424,4 +427,4 @@ class AdapterOptimizer:
         if out.dtype != torch.float32 or out.numel() < 1 or out.device != self.device:
             raise ValueError("the norm is written into an fp32 tensor on the gradients' device")
         ql.qlora_grad_norm(self.plan, self._plan_ptr, self.grad_scale if grad_scale is None else grad_scale, out,
-                           self._workspace_ptr, self._workspace_bytes, stream=stream)
+                           self._norm_workspace_ptr, self._workspace_bytes, stream=stream)

@@ -592,3 +592,41 @@ def test_tensor_of_more_than_two_to_the_31_weights():
         moved += int((w[at:at + 2 ** 28] != 0).sum())
     assert moved == count
     assert int((opt.tensors[0].exp_avg[n - 300:] != 0).sum()) == 300 and int((opt.tensors[0].exp_avg_sq[:300] != 0).sum()) == 300
+
+
+def test_a_norm_and_a_step_share_no_scratch(monkeypatch):
+    """A norm for a log line may run beside a step on another stream: the partial sums of the two lie apart."""
+    import torch
+    from paper_2306_08162_amd.device import AdapterOptimizer, OptimTensor
+    announce("adamw scratch of norm and step")
+    t = lambda n: torch.zeros(n, device="cuda:0")
+    opt = AdapterOptimizer([OptimTensor(t(8), t(8))], lr=1e-3, max_grad_norm=1.0)
+    seen = {}
+    monkeypatch.setattr(ql, "qlora_adamw_step", lambda *a, **kw: seen.__setitem__("step", a[-2:]))
+    monkeypatch.setattr(ql, "qlora_grad_norm", lambda *a, **kw: seen.__setitem__("norm", a[-2:]))
+    opt.step()
+    opt.grad_norm(t(1))
+    (a, na), (b, nb) = seen["step"], seen["norm"]
+    need = ql.qlora_optim_workspace_bytes()
+    assert min(na, nb) >= need and (a + need <= b or b + need <= a)
+
+
+def test_norms_beside_steps_on_another_stream():
+    import torch
+    announce("adamw norm on one stream, steps on another")
+    alone, both = (_Set(91, sizes=(300000, 70001, 5), param="bf16") for _ in range(2))
+    kw = dict(lr=1e-2, max_grad_norm=0.05, seed=2)
+    a, b = alone.optimizer(**kw), both.optimizer(**kw)
+    outs = [torch.zeros(1, device="cuda:0") for _ in range(20)]
+    torch.cuda.synchronize()
+    one, two = torch.cuda.Stream(), torch.cuda.Stream()
+    for out in outs:
+        a.step()
+        b.step(stream=one)
+        b.grad_norm(out, 0.5, stream=two)
+    torch.cuda.synchronize()
+    assert torch.equal(a.control, b.control)
+    for n in alone.buf:
+        assert torch.equal(alone.buf[n], both.buf[n]), n
+    norm = _norm(alone, 0.5)
+    assert all(abs(float(out) - norm) <= 1.01 * U * norm for out in outs)
