@@ -385,8 +385,8 @@ int qlora_lrec_loss_scaled(const void *student_logits, const void *teacher_logit
  *
  * logits may begin at any element (a slice of a larger tensor), stats is 16-byte aligned, the other pointers 4; V <= 2^28,
  * M < 2^22, M*V < 2^35, M*row_stride < 2^40.
- * workspace: qlora_token_logprobs_workspace_bytes(M, V, alternatives, dtype) bytes; NULL is accepted where that is 0
- * because rows are short (a call with bad arguments says so itself).  Calls that share a workspace and overlap in time
+ * workspace: qlora_token_logprobs_workspace_bytes(M, V, alternatives, dtype) bytes, enough for every call with fewer rows
+ * too; NULL is accepted where that is 0 because rows are short (a call with bad arguments says so itself).  Calls that share a workspace and overlap in time
  * (two streams, two captured graphs) race.  Sums run in a fixed order: results are bitwise reproducible.
  */
 #define QLORA_MAX_ALTERNATIVES 64

@@ -786,7 +786,7 @@ inline bool between_elements(const void *p, int dtype) { return reinterpret_cast
 size_t qlora_token_logprobs_workspace_bytes(int M, int V, int alternatives, int dtype)
 {
     if (check_logits(M, V, dtype) != QLORA_OK || alternatives < 0 || alternatives > QLORA_MAX_ALTERNATIVES) return 0;
-    const size_t bytes = score_workspace_bytes(M, V, alternatives, dtype);
+    const size_t bytes = score_workspace_bound(M, V, alternatives, dtype);
     return bytes ? round_up(bytes) : 0;
 }
 
@@ -804,7 +804,7 @@ int qlora_token_logprobs(const void *logits, int64_t row_stride, const int32_t *
     if (between_elements(logits, dtype) || misaligned(stats) || misaligned(workspace) || odd4(tokens) || odd4(logprob) ||
         odd4(entropy) || (alternatives > 0 && (odd4(alt_tokens) || odd4(alt_logprobs))))
         return QLORA_E_ALIGN;
-    const size_t need = qlora_token_logprobs_workspace_bytes(M, V, alternatives, dtype);
+    const size_t need = score_workspace_bytes(M, V, alternatives, dtype);
     if (need && (!workspace || workspace_bytes < need)) return QLORA_E_WORKSPACE;
     begin_call();
     launch_token_logprobs(logits, row_stride, tokens, logprob, entropy, alt_tokens, alt_logprobs, alternatives, stats, M, V,

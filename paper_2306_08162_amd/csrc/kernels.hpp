@@ -183,12 +183,14 @@ void launch_lrec_loss(const void *student, const void *teacher, const int32_t *l
 
 // logprob.hip -- log probabilities of given tokens, entropy and top alternatives of rows of logits, and the gradient.
 // dt: 0 fp16, 1 bf16, 2 fp32.  A row is taken in `splits` segments of `seg` 16-byte pieces, one workgroup of `threads`
-// each; with more than one the workspace holds their results (score_workspace_bytes; 0 with one).
+// each; with more than one the workspace holds their results (score_workspace_bytes; 0 with one).  score_workspace_bound is
+// enough for every number of rows up to M: few rows take more segments each, and a smaller batch could need more than a larger one.
 struct ScorePlan {
     int splits, seg, threads;
 };
 ScorePlan score_plan(int M, int V, int dt);
 size_t score_workspace_bytes(int M, int V, int k, int dt);
+size_t score_workspace_bound(int M, int V, int k, int dt);
 // tokens, logprob, entropy, stats ([M,4]: maximum, sum of exp(z - maximum), its logarithm, entropy) may be NULL
 void launch_token_logprobs(const void *logits, long stride, const int32_t *tokens, float *logprob, float *entropy,
                            int32_t *alt_tokens, float *alt_logprobs, int k, float *stats, int M, int V, int dt,

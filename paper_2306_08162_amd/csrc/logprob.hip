@@ -712,6 +712,15 @@ size_t score_workspace_bytes(int M, int V, int k, int dt)
     return p.splits == 1 ? 0 : (size_t)M * p.splits * (sizeof(float4_t) + sizeof(key_t) * k);
 }
 
+size_t score_workspace_bound(int M, int V, int k, int dt)
+{
+    if (score_plan(M, V, dt).splits == 1) return 0;                    // which follows from V alone
+    const size_t pieces = pieces_of(V, dt);
+    // of many rows each has ceil(pieces / SEGMENT) segments, of few no more than that or the spread of score_plan
+    const size_t many = M * ((pieces + SEGMENT - 1) / SEGMENT), few = std::min<size_t>(M * ((pieces + 2047) / 2048), 512);
+    return std::max(many, few) * (sizeof(float4_t) + sizeof(key_t) * k);
+}
+
 void launch_token_logprobs(const void *logits, long stride, const int32_t *tokens, float *logprob, float *entropy,
                            int32_t *alt_tokens, float *alt_logprobs, int k, float *stats, int M, int V, int dt,
                            void *workspace, hipStream_t s)

@@ -551,3 +551,17 @@ def test_rows_with_a_large_maximum(V, dtype):
         z[M + i, [5, V - 2]] = top
         z[2 * M + i, [7, V - 3]] = top, below
     _check_both(z, np.tile([V // 2, 5, V - 3], (M, 1)).T.ravel(), dtype, 3)
+
+
+def test_workspace_of_a_batch_serves_a_smaller_one():
+    """64 rows are taken in more segments than 100 are; what lies behind the larger batch's workspace stays as it was."""
+    import torch
+    announce("token logprobs workspace of 100 rows, 64 rows")
+    V, k = 100000, 20
+    need = ql.qlora_token_logprobs_workspace_bytes(100, V, k, ql.QLORA_F16)
+    c = _Call(_logits(70, 64, V, "f16"), _tokens(70, 64, V), "f16", k)
+    store = torch.full((need + 4096,), 0xA5, dtype=torch.uint8, device="cuda:0")
+    c.ws = store[:need]
+    c.forward()
+    c.check()
+    assert (store[need:] == 0xA5).all()

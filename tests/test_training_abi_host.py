@@ -167,3 +167,12 @@ def test_optimizer_refuses_tensors_in_host_memory():
     from paper_2306_08162_amd.device import AdapterOptimizer, OptimTensor
     with pytest.raises(ValueError):
         AdapterOptimizer([OptimTensor(torch.zeros(8), torch.zeros(8))], lr=1e-3)
+
+
+@pytest.mark.parametrize("V,dtype", [(100000, 0), (128259, 1), (65537, 0), (40000, 2), (50257, 2), (1 << 20, 0), (32000, 0)])
+def test_token_logprobs_workspace_of_a_batch_serves_its_smaller_ones(V, dtype):
+    """Never less for more rows or alternatives, none for one number of rows and some for another."""
+    sizes = [[ql.qlora_token_logprobs_workspace_bytes(M, V, k, dtype) for M in range(1, 700)] for k in (0, 5, 64)]
+    for row in sizes:
+        assert all(a <= b for a, b in zip(row, row[1:])) and len({n == 0 for n in row}) == 1
+    assert all(a <= b <= c for a, b, c in zip(*sizes))
