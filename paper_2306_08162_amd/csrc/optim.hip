@@ -25,6 +25,8 @@
 #include "common.hpp"
 #include "kernels.hpp"
 
+#include <cfloat>
+
 namespace qlora {
 
 namespace {
@@ -362,8 +364,17 @@ __device__ __forceinline__ void adam4(const AdamArgs &a, const AdamCoef &c, cons
         m[e] = m[e] + x * a.c1;
         v[e] = v[e] * a.b2 + (x * x) * a.c2;
         u[e] = __builtin_amdgcn_sqrtf(v[e]);
-        w[e] = w[e] * c.decay - c.rate * (m[e] * __builtin_amdgcn_rcpf(u[e] * c.root + a.eps));
     }
+    // the hardware's root takes what is below the smallest normal number for 0: those are brought up by a power of four first (a
+    // test of four weights together: few waves have such a v, and one of zeros alone finds zeros again)
+    if (fminf(fminf(v[0], v[1]), fminf(v[2], v[3])) < FLT_MIN) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (v[e] < FLT_MIN) u[e] = __builtin_amdgcn_sqrtf(v[e] * 0x1p64f) * 0x1p-32f;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        w[e] = w[e] * c.decay - c.rate * (m[e] * __builtin_amdgcn_rcpf(u[e] * c.root + a.eps));
 }
 
 // ALONE: this launch is the whole step (see adamw_alone_kernel)

@@ -630,3 +630,51 @@ def test_norms_beside_steps_on_another_stream():
         assert torch.equal(alone.buf[n], both.buf[n]), n
     norm = _norm(alone, 0.5)
     assert all(abs(float(out) - norm) <= 1.01 * U * norm for out in outs)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_second_moments_below_the_normal_numbers(bits):
+    """Gradients of 1.5e-19 to 3e-19: v lies below 2^-126, its root does not, and with a tiny eps the update is lr as for
+    any other gradient."""
+    announce(f"adamw tiny second moments bits={bits}")
+    sizes = (1000, 4097)
+    s = _Set(81, sizes=sizes, param="f32", bits=bits)
+    lr, eps, b1, b2, seed = 1e-2, 1e-30, 0.9, 0.98, 17
+    opt = s.optimizer(lr=lr, betas=(b1, b2), eps=eps, seed=seed)
+    first, codes_off = [0, 4], 0
+    for t in range(1, 4):
+        for i, n in enumerate(sizes):
+            x = wl.normal(900 + 10 * t + i, n)
+            s.put("grad", i, np.sign(x) * (1.5e-19 + 1.5e-19 * (np.abs(x) % 1.0)))
+        before = [{n: s.get(n, i) for n in s.buf} for i in range(len(sizes))]
+        opt.step()
+        for i, old in enumerate(before):
+            ratio, wd = s.hyper(i)
+            f = np.float32
+            g = old["grad"].astype(f)
+            if bits == 8:
+                m0 = ref.decode(old["exp_avg"], old["avg_scale"]).astype(f)
+                u0 = ref.decode(old["exp_avg_sq"], old["avg_sq_scale"]).astype(f)
+                v0 = u0 * u0
+                m, v = ref.moments_f32(m0, v0, g, b1, b2)
+                mc, uc, ms, us = ref.states8(m, v, ref.random_words(seed, t, first[i], sizes[i]))
+                np.testing.assert_array_equal(s.get("avg_scale", i), ms)
+                np.testing.assert_array_equal(s.get("avg_sq_scale", i), us)
+                np.testing.assert_array_equal(s.get("exp_avg", i), mc)
+                off = s.get("exp_avg_sq", i).astype(int) - uc
+                assert np.all(np.abs(off) <= 1)
+                codes_off += int((off != 0).sum())
+            else:
+                m0, v0 = old["exp_avg"], old["exp_avg_sq"]
+            w, m, v = ref.step(old["param"], m0, v0, g, lr=lr * ratio, beta1=b1, beta2=b2, eps=eps, weight_decay=wd, t=t)
+            # Below 2^-126 a product is off by half a unit of 2^-149: v by two of them and by that of u0 u0 (8 bits)
+            v_off = 2.0 ** -149 * 1.5 + 6 * U * v
+            assert v.max() < 2.0 ** -126 and v.min() > 2.0 ** -132
+            if bits == 32:
+                assert np.all(np.abs(s.get("exp_avg_sq", i) - v) <= v_off)
+            # ... the root by half of that relative to v; the rest as for ordinary gradients
+            spread = lr * ratio / (1 - b1 ** t) * (np.abs(b1 * m0) + np.abs((1 - b1) * g)) / (np.sqrt(v / (1 - b2 ** t)) + eps)
+            bound = (64 * U + 0.51 * v_off / v) * spread + 3 * U * np.abs(old["param"])
+            assert np.all(np.abs(s.get("param", i) - w) <= bound)
+    assert codes_off <= 8 + 3 * sum(sizes) / 2 ** 17
+    s.untouched_between()
