@@ -13,7 +13,7 @@
 //
 // A token that is almost certain has p = 1 / (1 + s) with a tiny s, and S = 1 + s would round it away: the sums keep
 // the entries equal to the maximum as a count n apart from the sum s of all others, ln S = log1p(s) where n = 1, and
-// log p and H of such a row keep their relative accuracy.
+// log p and H of such a row keep their relative accuracy.  So does the gradient at the token, g (1 - p) = -g expm1(log p).
 //
 // Alternatives.  Of its lanes' largest entries each of a workgroup's w waves finds (nearly) the ceil(k / w)-th, by bisection
 // with ballots; at least k entries are not below tau, the smallest of the w, and on rows in no special order not many more.
@@ -598,7 +598,8 @@ __global__ __launch_bounds__(GT) void score_grad_kernel(const ScoreGradArgs a)
     const float g = given && a.d_logprob ? a.d_logprob[row] : 0.f, h = a.d_entropy ? a.d_entropy[row] : 0.f;
     const bool nothing = g == 0.f && h == 0.f;                         // a row of zeros, whatever its logits
     const float4_t st = a.stats[row];
-    const float m = st[0], inv = 1.f / st[1], c = h * (st[3] - st[2]) + g, hl = h * LN2;   // g + h (log p + H) = hl x + c
+    const float m = st[0], inv = 1.f / st[1], hl = h * LN2;
+    const float ch = h * (st[3] - st[2]), c = ch + g;                  // h (log p + H) = hl x + ch
     Piece<DT> r[GCH];
     if (!nothing) {
 #pragma unroll
@@ -622,9 +623,20 @@ __global__ __launch_bounds__(GT) void score_grad_kernel(const ScoreGradArgs a)
             o[e] = nothing ? 0.f : -(exp2_hw(x) * inv) * fmaf(hl, fmaxf(x, NOTHING), c);
         }
         if (given && t / E == p) {
+            float zt = r[i].val(0), o_t = o[0];
 #pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (t % E == e) o[e] += g;
+            for (int e = 1; e < E; ++e) {
+                zt = t % E == e ? r[i].val(e) : zt;
+                o_t = t % E == e ? o[e] : o_t;
+            }
+            const float x = (zt - m) * LOG2E, p_t = exp2_hw(x) * inv;
+            // g (1 - p): as a difference while that rounds once, by log p where the difference would lose digits
+            if (nothing || p_t < 0.5f)
+                o_t += g;
+            else
+                o_t = -g * expm1f((zt - m) - st[2]) - p_t * fmaf(hl, fmaxf(x, NOTHING), ch);
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] = t % E == e ? o_t : o[e];
         }
         u32x4_t w;
         if constexpr (DT == 2) {

@@ -565,3 +565,24 @@ def test_workspace_of_a_batch_serves_a_smaller_one():
     c.forward()
     c.check()
     assert (store[need:] == 0xA5).all()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+def test_gradients_of_almost_certain_tokens_keep_their_digits(dtype):
+    """g (1 - p) of a dominant token, where p rounds to 1; and that of a token which another one dominates."""
+    announce(f"token logprobs gradient, almost certain {dtype}")
+    V = 32000
+    z = np.zeros((5, V))
+    for row, top in enumerate((20.0, 25.0, 30.0, 40.0, 30.0)):
+        z[row, 100 * row] = top
+    c = _Call(z, [0, 100, 200, 300, 401], dtype, 0)
+    c.forward()
+    g = np.array([1024.0, -1024.0, 4096.0, 2.0 ** 30, 3.0])
+    c.backward(g, None)
+    at = (np.arange(5), c.tokens_h)
+    want = -g * np.expm1(scoring.score(z, c.tokens_h, 0)[0])           # (1 - p in 64 bits is off by 2^-54: half a step of fp16 at 40)
+    got = c.dlogits.double().cpu().numpy()[at]
+    # log p is off by 300 u (see the test of the scores), a difference carries that over with a factor of at most 1, and expm1
+    # and the product add a few more
+    bound = (310 * U + HALF_ULP[dtype]) * 1.01 * np.abs(want) + TINY[dtype]
+    assert np.all(np.abs(got - want) <= bound), np.abs(got - want) / bound
