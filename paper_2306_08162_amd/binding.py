@@ -175,12 +175,60 @@ def _ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
-def _rows_ptr(t) -> Optional[int]:
-    """Pointer of a matrix whose rows may lie further apart than they are long (the call is handed the distance)."""
+# What the calls on token scores are handed as tensors is held against their arguments: a pointer says neither type nor size,
+# and 64-bit tokens, which torch makes by default, would be read as pairs of 32-bit ones.  (Raw integer pointers pass as they are.)
+_SCORE_TYPES = None             # torch's int32, float32 and the types behind QLORA_F16, QLORA_BF16, QLORA_F32
+
+
+def _score_types():
+    global _SCORE_TYPES
+    import torch
+    _SCORE_TYPES = torch.int32, torch.float32, (torch.float16, torch.bfloat16, torch.float32)
+    return _SCORE_TYPES
+
+
+def _reach(t) -> int:
+    """Entries from a tensor's first to the end of its memory."""
+    return t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
+
+
+def _refuse(t, dtype, count: int, device: int, name: str) -> None:
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} holds {t.dtype}, the call takes {dtype}")
+    if not t.is_contiguous():
+        raise ValueError("qlora buffers must be contiguous")
+    if t.numel() < count and _reach(t) < count:
+        raise ValueError(f"{name} has {t.numel()} entries where the call takes {count}")
+    _on_current_device(t, device, name)
+
+
+def _on_current_device(t, device: int, name: str) -> None:
+    if t.get_device() != device and t.get_device() != _current_device():
+        raise ValueError(f"{name} lives on {t.device}, which is not the current GPU")
+
+
+def _entries_ptr(t, dtype, count: int, device: int, name: str) -> Optional[int]:
+    """Pointer of `count` contiguous entries of dtype; device: the current one, or -2 while that is not known."""
     if t is None or isinstance(t, int):
         return t
-    if t.dim() > 0 and t.shape[-1] > 1 and t.stride(-1) != 1:
+    if t.dtype is not dtype or t.numel() < count or t.get_device() != device or not t.is_contiguous():
+        _refuse(t, dtype, count, device, name)
+    return t.data_ptr()
+
+
+def _rows_ptr(t, dtype, extent: int, device: int, name: str) -> Optional[int]:
+    """Pointer of a matrix whose rows may lie further apart than they are long (the call is handed the distance); from the first
+    entry to the last there are `extent`.  16-bit patterns may travel as integers.  dtype None: not a known one."""
+    if t is None or isinstance(t, int):
+        return t
+    if dtype is not None and t.dtype is not dtype and (t.dtype.is_floating_point or t.element_size() != dtype.itemsize):
+        raise ValueError(f"{name} holds {t.dtype}, the call was told {dtype}")
+    if not t.is_contiguous() and t.shape[-1] > 1 and t.stride(-1) != 1:
         raise ValueError("the entries of a row must be contiguous")
+    if t.numel() < extent and _reach(t) < extent:
+        raise ValueError(f"{name} ends before its last row does")
+    if t.get_device() != device:
+        _on_current_device(t, device, name)
     return t.data_ptr()
 
 
@@ -211,12 +259,22 @@ def _current_stream() -> int:
     return current
 
 
+def _current_device() -> int:
+    import torch
+    return torch.cuda.current_device() if torch.cuda.is_available() else -2         # no tensor's
+
+
 def _stream(stream) -> Optional[int]:
     if stream is None:
         return _current_stream() or None
     if isinstance(stream, int):
         return stream or None
     return stream.cuda_stream or None
+
+
+def _stream_at(stream, device: int) -> Optional[int]:
+    """_stream for callers that have asked for the current device already."""
+    return _raw_stream[0](device) or None if stream is None and _raw_stream else _stream(stream)
 
 
 def _nbytes(t) -> int:
@@ -545,11 +603,29 @@ def qlora_token_logprobs_workspace_bytes(M: int, V: int, alternatives: int, dtyp
 def qlora_token_logprobs(logits, row_stride: int, tokens, logprob, entropy, alt_tokens, alt_logprobs, alternatives: int,
                          stats, M: int, V: int, dtype: int, workspace, workspace_bytes: Optional[int] = None,
                          stream=None, check: bool = True) -> int:
-    if workspace_bytes is None:
-        workspace_bytes = _nbytes(workspace)
-    st = load().qlora_token_logprobs(_rows_ptr(logits), row_stride, _ptr(tokens), _ptr(logprob), _ptr(entropy),
-                                     _ptr(alt_tokens), _ptr(alt_logprobs), alternatives, _ptr(stats), M, V, dtype,
-                                     _ptr(workspace), workspace_bytes, _stream(stream))
+    i32, f32, floats = _SCORE_TYPES or _score_types()
+    here = _raw_stream[1]() if _raw_stream else -2
+    z = _rows_ptr(logits, floats[dtype] if 0 <= dtype < 3 else None, (M - 1) * row_stride + V, here, "logits")
+    tokens = None if logprob is None else _entries_ptr(tokens, i32, M, here, "tokens")
+    logprob = None if logprob is None else _entries_ptr(logprob, f32, M, here, "logprob")
+    entropy = None if entropy is None else _entries_ptr(entropy, f32, M, here, "entropy")
+    if alternatives > 0:
+        alt_tokens = _entries_ptr(alt_tokens, i32, M * alternatives, here, "alt_tokens")
+        alt_logprobs = _entries_ptr(alt_logprobs, f32, M * alternatives, here, "alt_logprobs")
+    else:
+        alt_tokens = alt_logprobs = None
+    stats = None if stats is None else _entries_ptr(stats, f32, 4 * M, here, "stats")
+    scratch = workspace
+    if workspace is None or isinstance(workspace, int):
+        workspace_bytes = workspace_bytes or 0
+    else:
+        scratch = _ptr(workspace)
+        if workspace.get_device() != here:
+            _on_current_device(workspace, here, "workspace")
+        if workspace_bytes is None:
+            workspace_bytes = workspace.numel() * workspace.element_size()
+    st = (_lib or load()).qlora_token_logprobs(z, row_stride, tokens, logprob, entropy, alt_tokens, alt_logprobs, alternatives, stats,
+                                               M, V, dtype, scratch, workspace_bytes, _stream_at(stream, here))
     if check and st != 0:
         raise QLoraError(st, "qlora_token_logprobs")
     return st
@@ -557,8 +633,16 @@ def qlora_token_logprobs(logits, row_stride: int, tokens, logprob, entropy, alt_
 
 def qlora_token_logprobs_bwd(logits, row_stride: int, tokens, stats, d_logprob, d_entropy, dlogits, d_row_stride: int,
                              M: int, V: int, dtype: int, stream=None, check: bool = True) -> int:
-    st = load().qlora_token_logprobs_bwd(_rows_ptr(logits), row_stride, _ptr(tokens), _ptr(stats), _ptr(d_logprob),
-                                         _ptr(d_entropy), _rows_ptr(dlogits), d_row_stride, M, V, dtype, _stream(stream))
+    i32, f32, floats = _SCORE_TYPES or _score_types()
+    held, here = floats[dtype] if 0 <= dtype < 3 else None, _raw_stream[1]() if _raw_stream else -2
+    z = _rows_ptr(logits, held, (M - 1) * row_stride + V, here, "logits")
+    dz = _rows_ptr(dlogits, held, (M - 1) * d_row_stride + V, here, "dlogits")
+    tokens = None if d_logprob is None else _entries_ptr(tokens, i32, M, here, "tokens")
+    stats = _entries_ptr(stats, f32, 4 * M, here, "stats")
+    d_logprob = None if d_logprob is None else _entries_ptr(d_logprob, f32, M, here, "d_logprob")
+    d_entropy = None if d_entropy is None else _entries_ptr(d_entropy, f32, M, here, "d_entropy")
+    st = (_lib or load()).qlora_token_logprobs_bwd(z, row_stride, tokens, stats, d_logprob, d_entropy, dz, d_row_stride, M, V, dtype,
+                                                   _stream_at(stream, here))
     if check and st != 0:
         raise QLoraError(st, "qlora_token_logprobs_bwd")
     return st

@@ -176,3 +176,76 @@ def test_token_logprobs_workspace_of_a_batch_serves_its_smaller_ones(V, dtype):
     for row in sizes:
         assert all(a <= b for a, b in zip(row, row[1:])) and len({n == 0 for n in row}) == 1
     assert all(a <= b <= c for a, b, c in zip(*sizes))
+
+
+def _tensors(M=4, V=64, k=5):
+    import torch
+    f32 = lambda *shape: torch.zeros(shape)
+    return dict(z=torch.zeros((M, V), dtype=torch.float16), tok=torch.zeros(M, dtype=torch.int32), lp=f32(M), ent=f32(M),
+                at=torch.zeros((M, k), dtype=torch.int32), alp=f32(M, k), stats=f32(M, 4), ws=torch.zeros(64, dtype=torch.uint8))
+
+
+@pytest.mark.parametrize("name,dtype", [("tok", "int64"), ("lp", "float16"), ("ent", "float64"), ("at", "int64"), ("alp", "bfloat16"),
+                                        ("stats", "float16"), ("z", "bfloat16"), ("z", "float32"), ("z", "uint8"), ("z", "int32")])
+def test_token_logprobs_refuses_tensors_of_other_types(name, dtype):
+    import torch
+    t = _tensors()
+    t[name] = t[name].to(getattr(torch, dtype))
+    with pytest.raises(ValueError, match="holds torch." + dtype):
+        _score(**{name: t[name]})
+
+
+@pytest.mark.parametrize("name", ["tok", "lp", "ent", "at", "alp", "stats", "z"])
+def test_token_logprobs_refuses_tensors_that_are_too_short(name):
+    t = _tensors()
+    short = t[name].flatten()[1:].clone()
+    with pytest.raises(ValueError, match="entries|ends before"):
+        _score(**{name: short})
+    with pytest.raises(ValueError, match="current GPU"):            # one entry further back in memory that is long enough
+        _score(**{name: t[name].flatten()[:-1]})
+
+
+def test_token_logprobs_refuses_rows_that_pass_the_end():
+    import torch
+    t = _tensors()
+    with pytest.raises(ValueError, match="ends before"):
+        _score(z=t["z"], stride=65)
+    wide = torch.zeros((4, 70), dtype=torch.float16)[:, :64]        # ... and takes a slice, 16-bit patterns as integers
+    for z in (wide, wide.view(torch.int16)):
+        with pytest.raises(ValueError, match="current GPU"):
+            _score(z=z, stride=70)
+    with pytest.raises(ValueError, match="a row must be contiguous"):
+        _score(z=torch.zeros((64, 4), dtype=torch.float16).T)
+
+
+@pytest.mark.parametrize("keep", ["z", "tok", "lp", "ent", "at", "alp", "stats", "ws"])
+def test_token_logprobs_refuses_tensors_in_host_memory(keep):
+    with pytest.raises(ValueError, match="current GPU"):
+        _score(**{keep: _tensors()[keep]})
+
+
+def test_token_logprobs_ignores_what_is_not_asked_for():
+    """Tokens beside no logprob, alternatives beside a count of 0: not looked at, so the refusal is that of the workspace."""
+    import torch
+    wrong = torch.zeros(1, dtype=torch.int64)
+    a = dict(V=1 << 20, stride=1 << 20, ws=None)
+    assert _score(tok=wrong, lp=None, **a) == E["QLORA_E_WORKSPACE"]
+    assert _score(at=wrong, alp=wrong, k=0, **a) == E["QLORA_E_WORKSPACE"]
+
+
+@pytest.mark.parametrize("name,dtype", [("tok", "int64"), ("stats", "float64"), ("g", "float16"), ("h", "float64"), ("z", "float32"),
+                                        ("dz", "bfloat16")])
+def test_token_logprobs_bwd_refuses_tensors_that_do_not_fit(name, dtype):
+    import torch
+    M, V = 4, 64
+    t = dict(z=torch.zeros((M, V), dtype=torch.float16), tok=torch.zeros(M, dtype=torch.int32), stats=torch.zeros((M, 4)),
+             g=torch.zeros(M), h=torch.zeros(M), dz=torch.zeros((M, V), dtype=torch.float16))
+    fake = dict(z=FAKE, tok=FAKE, stats=FAKE, g=FAKE, h=FAKE, dz=0x20000)
+    call = lambda a: ql.qlora_token_logprobs_bwd(a["z"], V, a["tok"], a["stats"], a["g"], a["h"], a["dz"], V, M, V, ql.QLORA_F16,
+                                                 stream=0, check=False)
+    with pytest.raises(ValueError, match="holds torch." + dtype):
+        call(fake | {name: t[name].to(getattr(torch, dtype))})
+    with pytest.raises(ValueError, match="entries|ends before"):
+        call(fake | {name: t[name].flatten()[1:].clone()})
+    with pytest.raises(ValueError, match="current GPU"):
+        call(fake | {name: t[name]})
