@@ -480,12 +480,11 @@ int qlora_grad_norm(const void *plan, const void *plan_device, float grad_scale,
  * One step.  max_grad_norm > 0: the norm is taken first, control->grad_norm receives it, the gradients are scaled
  * by clip = min(1, max_grad_norm / norm), and if the norm is not finite (an overflow under loss scaling), or not below 2^63
  * after clipping (exp_avg_sq would overflow), nothing changes but control->skipped and grad_norm; INFINITY checks without
- * clipping.  max_grad_norm == 0: neither; the workspace
- * may then be NULL, clip is 1, and a gradient that is not finite makes its weight and states NaN (8-bit states: its
- * block's); one above 1.8e19, whose square is not finite, overflows exp_avg_sq.  Gradients are not cleared.  QLORA_E_VALUE: a beta outside [0, 1), max_grad_norm negative or NaN, eps not
- * between 2^-126 and the largest fp32 number.
- * Calls that share a control block or a workspace and overlap in time race.  Two launches;
- * one where max_grad_norm is 0 and the plan small.
+ * clipping.  max_grad_norm == 0: neither; the workspace may then be NULL, clip is 1, and a gradient that is not finite makes
+ * its weight and states NaN (8-bit states: its block's); one above 1.8e19, whose square is not finite, overflows exp_avg_sq.
+ * Gradients are not cleared.  QLORA_E_VALUE: a beta outside [0, 1), max_grad_norm negative or NaN, eps not between 2^-126 and
+ * the largest fp32 number.  Calls that share a control block or a workspace, qlora_grad_norm among them, and overlap in time
+ * race.  Two launches; one where max_grad_norm is 0 and the plan small.
  */
 int qlora_adamw_step(const void *plan, const void *plan_device, qlora_optim_control_t *control, double beta1, double beta2,
                      double eps, double max_grad_norm, void *workspace, size_t workspace_bytes, void *stream);

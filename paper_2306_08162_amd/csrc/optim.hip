@@ -5,8 +5,8 @@
 //
 // The step is bound by HBM: with fp32 gradients and 16-bit weights 24 bytes a weight (fp32 states), 12 with states of
 // 8 bits, and 4 more for the norm.  20M weights with fp32 masters: 103 us with the norm, 5.8 TB/s of the 600 MB that a step
-// cannot do without (a large copy reaches 4.9 to 5.7); 160M with 8-bit states: 435 us, 5.9 TB/s with the second reading of the
-// gradients counted, and 61 instructions a weight close behind it.
+// cannot do without (a large copy reaches 4.9 to 5.7); 160M with 8-bit states: 434 us, 5.9 TB/s with the second reading of the
+// gradients counted, and 62 instructions a weight close behind it.
 // A plan in device memory has a record for each chunk of up to 2048 weights of a tensor, one workgroup's work: hundreds of small
 // matrices fill the chip like one large one.  (Chunks of 1024 and 4096: 517 and 481 us where 2048 took 485 on those 160M, but 22.3
 // and 25.8 where it took 22.1 on 5M in 96 tensors.)
